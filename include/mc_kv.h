@@ -326,6 +326,128 @@ mc_status mc_kv_fork_sequence(void* alloc, const int32_t* parent_pages /* host *
 mc_status mc_kv_copy_page(const mc_pool_desc* pool, int32_t layer_begin, int32_t layer_end,
                           int32_t src_page, int32_t dst_page, int32_t slots, void* stream);
 
+/* ---- KV cache in 8 bits --------------------------------------------------------
+ * A page pool of half the bytes: decode steps are bound by reading K/V, transfers
+ * by the bytes they move, the number of sequences by the memory of their pages.
+ * Every element is an e4m3 code (1 sign, 4 exponent, 3 mantissa bits; largest 448,
+ * no infinities); the 16 tokens of K, or of V, of one kv head in one page form a
+ * block, which has one scale, a power of two:  value = code x scale.
+ *
+ *   codes   [layer][page][2: 0=K 1=V][kv_head][2048 bytes]
+ *           a K block is [slot][D], a V block [D][slot] (transposed)
+ *   scales  [layer][page][kv_head][2: 0=K 1=V]  float32
+ *
+ * The scale of a block is 2^k with the least k for which the largest finite
+ * magnitude among its tokens is at most 448 x 2^k, but at least 2^-15 in a pool of
+ * fp16 tokens and 2^-100 in one of bf16, and at most 2^8 and 2^120: code x scale is
+ * then always exactly a number of the pool's 16-bit type.  Values are rounded to
+ * the nearest code, ties to even; at the largest scale those beyond 240 x scale
+ * become that (61440 for fp16).  NaN and infinities become NaN codes and do not
+ * count for the scale.  Whatever else writes a pool must leave such scales.
+ *
+ * dtype is the 16-bit type of k_new, v_new, q and out.  codes is 16-byte, scales
+ * 8-byte aligned.  Errors, streams, page tables, bounds checks and the counter of
+ * what was skipped (mc_kv8_copy_check; a page counts once) are as above. */
+typedef struct {
+  void* codes;
+  float* scales;
+  int32_t num_layers;
+  int32_t num_pages;
+  int32_t page_size;    /* must be 16 */
+  int32_t num_kv_heads;
+  int32_t head_dim;     /* must be 128 */
+  int32_t dtype;        /* mc_dtype */
+  int32_t* skipped;     /* device int32 counter, 4-byte aligned, or NULL */
+} mc_pool8_desc;
+
+mc_status mc_kv8_copy_check(const mc_pool8_desc* pool, int32_t* skipped_out /* host */,
+                            void* stream);
+
+/* mc_kv_append into an 8-bit pool.  In a page whose first new token is at slot 0 the
+ * scale is the new tokens'.  Behind earlier tokens it is the larger of the block's
+ * own and the new tokens'; if it grows, the codes of the slots before the first new
+ * token are rounded to it.  Slots behind the last new token keep their bytes and
+ * count as empty from then on.  Two sequences of one call must not append to one
+ * page.  A sequence with a negative begin is skipped, and every token counted. */
+mc_status mc_kv8_append(const mc_pool8_desc* pool, int32_t layer,
+                        const void* k_new /* device [total_q][Hkv][D] */,
+                        const void* v_new /* device [total_q][Hkv][D] */,
+                        int32_t batch, int32_t total_q,
+                        const int32_t* cu_q /* device [batch+1] */,
+                        const int32_t* begin /* device [batch] */,
+                        const int32_t* page_table /* device */,
+                        const int32_t* cu_pages /* device [batch+1] */, void* stream);
+
+/* mc_attn_plan and mc_prefix_prefill_attn over an 8-bit pool: out and lse of the formula
+ * above with K and V = code x scale, in one ragged batch of ranges and single tokens;
+ * a key that a row must not see, and slots behind a sequence's last token, have no
+ * influence on it whatever they hold.  The plan divides the KV tiles of all q tiles
+ * evenly among the workgroups that the GPU runs at a time; q tiles that it cuts are
+ * combined before the call returns control of the stream.  Plan, workspace and
+ * ahead_tokens follow the rules of mc_attn_plan and mc_attn_plan_ahead, and calls that
+ * use one workspace must run one after the other; but a sequence whose offsets,
+ * table or page ids are malformed is left out by itself (its out and lse rows are
+ * not written) and the others are computed; mc_attn8_plan_check then returns
+ * MC_ERR_RANGE.  The two kinds of plan are not interchangeable. */
+size_t mc_attn8_workspace_size(int32_t batch, int32_t total_q, int32_t num_q_heads,
+                               int32_t num_kv_heads);
+mc_status mc_attn8_plan(const mc_pool8_desc* pool, int32_t num_q_heads, int32_t batch,
+                        int32_t total_q, const int32_t* cu_q, const int32_t* begin,
+                        const int32_t* page_table, const int32_t* cu_pages,
+                        void* workspace /* device */, size_t workspace_bytes, void* stream);
+mc_status mc_attn8_plan_ahead(const mc_pool8_desc* pool, int32_t num_q_heads, int32_t batch,
+                              int32_t total_q, const int32_t* cu_q, const int32_t* begin,
+                              const int32_t* page_table, const int32_t* cu_pages,
+                              int32_t ahead_tokens, void* workspace /* device */,
+                              size_t workspace_bytes, void* stream);
+mc_status mc_attn8_plan_check(const void* workspace /* device */, void* stream);
+mc_status mc_prefix_prefill_attn8(const mc_pool8_desc* pool, int32_t layer,
+                                  const void* q /* device [total_q][Hq][D] */,
+                                  int32_t num_q_heads, int32_t batch, int32_t total_q,
+                                  const int32_t* cu_q, const int32_t* begin,
+                                  const int32_t* page_table, const int32_t* cu_pages,
+                                  float sm_scale /* 0 -> 1/sqrt(D) */,
+                                  void* out /* device [total_q][Hq][D], pool dtype */,
+                                  float* lse /* device [total_q][Hq] */, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* A token range of one sequence between a 16-bit pool and an 8-bit one of the same
+ * dtype and kv heads, layers [layer_begin, layer_end) of both; each pool has its own
+ * table of the sequence (device, must cover token s1-1).
+ *   compress: tokens [s0, s1), s0 a multiple of 16 (MC_ERR_RANGE otherwise): every block
+ *     of the range gets the scale of its tokens in the range; the slots behind s1 of
+ *     the last page keep their bytes.
+ *   restore:  the slots of tokens [s0, s1), any s0, get code x scale (exactly).
+ * What has a page id outside its pool is skipped and counted in the pool written to. */
+mc_status mc_kv8_compress_range(const mc_pool_desc* pool, const mc_pool8_desc* pool8,
+                                int32_t layer_begin, int32_t layer_end,
+                                const int32_t* pages /* device, of pool */, int32_t n_pages,
+                                const int32_t* pages8 /* device, of pool8 */, int32_t n_pages8,
+                                int32_t s0, int32_t s1, void* stream);
+mc_status mc_kv8_restore_range(const mc_pool8_desc* pool8, const mc_pool_desc* pool,
+                               int32_t layer_begin, int32_t layer_end,
+                               const int32_t* pages8 /* device, of pool8 */, int32_t n_pages8,
+                               const int32_t* pages /* device, of pool */, int32_t n_pages,
+                               int32_t s0, int32_t s1, void* stream);
+
+/* mc_kv_pack_range and mc_kv_unpack_range of an 8-bit pool.  A scale belongs to a whole
+ * page, so pages move whole: s0 must be a multiple of 16 (MC_ERR_RANGE otherwise),
+ * and the last page's slots behind s1 move with it.  With n pages in the range,
+ *   sendbuf  codes [layer - layer_begin][page - s0/16][2][kv_head][2048], then
+ *            scales [layer - layer_begin][page - s0/16][kv_head][2] float32:
+ *            (layer_end - layer_begin) n kv_heads (4096 + 8) bytes. */
+mc_status mc_kv8_pack_range(const mc_pool8_desc* pool, int32_t layer_begin, int32_t layer_end,
+                            const int32_t* pages /* device */, int32_t n_table_pages, int32_t s0,
+                            int32_t s1, void* sendbuf /* device, 16-byte aligned */, void* stream);
+mc_status mc_kv8_unpack_range(const mc_pool8_desc* pool, int32_t layer_begin, int32_t layer_end,
+                              const int32_t* pages /* device */, int32_t n_table_pages, int32_t s0,
+                              int32_t s1, const void* sendbuf /* device */, void* stream);
+
+/* mc_kv_copy_page of an 8-bit pool: the copy that mc_kv_fork_sequence leaves to be made.
+ * The whole page and its scales. */
+mc_status mc_kv8_copy_page(const mc_pool8_desc* pool, int32_t layer_begin, int32_t layer_end,
+                           int32_t src_page, int32_t dst_page, void* stream);
+
 /* ---- host arithmetic of remote_send ------------------------------------------
  * Which token ranges a sender copies, computes and sends (Sec. 3.5, the two
  * prefix-matching cases of the attention/transfer interface).  The sender's

@@ -28,6 +28,9 @@ EXPORTS = [
     "mc_plan_remote_send", "mc_addr_compress", "mc_addr_expand",
     "mc_prefix_index_create", "mc_prefix_index_destroy", "mc_prefix_index_insert",
     "mc_prefix_index_match", "mc_prep_recv", "mc_kv_fork_sequence", "mc_kv_copy_page",
+    "mc_kv8_append", "mc_kv8_copy_check", "mc_attn8_workspace_size", "mc_attn8_plan", "mc_attn8_plan_ahead",
+    "mc_attn8_plan_check", "mc_prefix_prefill_attn8", "mc_kv8_compress_range", "mc_kv8_restore_range",
+    "mc_kv8_pack_range", "mc_kv8_unpack_range", "mc_kv8_copy_page",
 ]
 
 
@@ -52,6 +55,12 @@ class mc_pool_desc(C.Structure):
                 ("dtype", C.c_int32), ("skipped", C.c_void_p)]
 
 
+class mc_pool8_desc(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("num_layers", C.c_int32),
+                ("num_pages", C.c_int32), ("page_size", C.c_int32), ("num_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("skipped", C.c_void_p)]
+
+
 class _LazyCalls:
     """Stands in for the native module until the first call that needs it."""
 
@@ -63,6 +72,7 @@ class _LazyCalls:
             _build.build_calls()
         native = importlib.import_module("._calls", __package__)
         native.setup(mc_pool_desc, C.c_void_p, C.c_int32, C.c_size_t, McArgumentError)
+        native.setup8(mc_pool8_desc)
         _calls = native
         return getattr(native, name)
 
@@ -120,6 +130,21 @@ def lib():
     L.mc_kv_fork_sequence.argtypes = [vp, C.POINTER(i32), i32, C.POINTER(i32), C.POINTER(i32),
                                       C.POINTER(i32), C.POINTER(i32)]
     L.mc_kv_copy_page.argtypes = [pd, i32, i32, i32, i32, i32, vp]
+    p8 = C.POINTER(mc_pool8_desc)
+    L.mc_kv8_append.argtypes = [p8, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    L.mc_kv8_copy_check.argtypes = [p8, C.POINTER(i32), vp]
+    L.mc_attn8_workspace_size.argtypes = [i32, i32, i32, i32]
+    L.mc_attn8_workspace_size.restype = sz
+    L.mc_attn8_plan.argtypes = [p8, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+    L.mc_attn8_plan_ahead.argtypes = [p8, i32, i32, i32, vp, vp, vp, vp, i32, vp, sz, vp]
+    L.mc_attn8_plan_check.argtypes = [vp, vp]
+    L.mc_prefix_prefill_attn8.argtypes = [p8, i32, vp, i32, i32, i32, vp, vp, vp, vp, C.c_float,
+                                          vp, vp, vp, sz, vp]
+    L.mc_kv8_compress_range.argtypes = [pd, p8, i32, i32, vp, i32, vp, i32, i32, i32, vp]
+    L.mc_kv8_restore_range.argtypes = [p8, pd, i32, i32, vp, i32, vp, i32, i32, i32, vp]
+    L.mc_kv8_pack_range.argtypes = [p8, i32, i32, vp, i32, i32, i32, vp, vp]
+    L.mc_kv8_unpack_range.argtypes = [p8, i32, i32, vp, i32, i32, i32, vp, vp]
+    L.mc_kv8_copy_page.argtypes = [p8, i32, i32, i32, i32, vp]
     _lib = L
     return L
 
@@ -168,6 +193,14 @@ def pool_desc(base, num_layers, num_pages, num_kv_heads, dtype, page_size=16, he
     """skipped: optional device int32 counter (zeroed by the caller) for mc_kv_copy_check."""
     return mc_pool_desc(_ptr(base), num_layers, num_pages, page_size, num_kv_heads, head_dim, dtype,
                         _ptr(skipped))
+
+
+def pool8_desc(codes, scales, num_layers, num_pages, num_kv_heads, dtype, page_size=16, head_dim=128,
+               skipped=None):
+    """A pool in 8 bits; dtype is the 16-bit type of the tokens.  skipped as in pool_desc, for
+    mc_kv8_copy_check."""
+    return mc_pool8_desc(_ptr(codes), _ptr(scales), num_layers, num_pages, page_size, num_kv_heads,
+                         head_dim, dtype, _ptr(skipped))
 
 
 # ---- allocator (host) ---------------------------------------------------------
@@ -349,3 +382,76 @@ def mc_kv_copy_page(pool: mc_pool_desc, layer_begin, layer_end, src_page, dst_pa
                     stream=None):
     _check(_calls.copy_page(pool, layer_begin, layer_end, src_page, dst_page, slots, stream),
            "mc_kv_copy_page")
+
+
+# ---- KV cache in 8 bits ---------------------------------------------------------
+def mc_kv8_copy_check(pool: mc_pool8_desc, stream=None) -> int:
+    """(status, skipped), as mc_kv_copy_check."""
+    n = C.c_int32(0)
+    st = lib().mc_kv8_copy_check(C.byref(pool), C.byref(n), _stream(stream))
+    if st not in (MC_OK, MC_ERR_RANGE):
+        raise McError(st, "mc_kv8_copy_check")
+    return st, n.value
+
+
+def mc_kv8_append(pool: mc_pool8_desc, layer, k_new, v_new, batch, total_q, cu_q, begin,
+                  page_table, cu_pages, stream=None):
+    _check(_calls.append8(pool, layer, k_new, v_new, batch, total_q, cu_q, begin, page_table,
+                          cu_pages, stream), "mc_kv8_append")
+
+
+def mc_attn8_workspace_size(batch, total_q, num_q_heads, num_kv_heads) -> int:
+    return lib().mc_attn8_workspace_size(batch, total_q, num_q_heads, num_kv_heads)
+
+
+def mc_attn8_plan(pool: mc_pool8_desc, num_q_heads, batch, total_q, cu_q, begin, page_table,
+                  cu_pages, workspace, workspace_bytes, stream=None):
+    _check(_calls.plan8(pool, num_q_heads, batch, total_q, cu_q, begin, page_table, cu_pages, 0,
+                        workspace, workspace_bytes, stream), "mc_attn8_plan")
+
+
+def mc_attn8_plan_ahead(pool: mc_pool8_desc, num_q_heads, batch, total_q, cu_q, begin, page_table,
+                        cu_pages, ahead_tokens, workspace, workspace_bytes, stream=None):
+    _check(_calls.plan8(pool, num_q_heads, batch, total_q, cu_q, begin, page_table, cu_pages,
+                        ahead_tokens, workspace, workspace_bytes, stream), "mc_attn8_plan_ahead")
+
+
+def mc_attn8_plan_check(workspace, stream=None):
+    _check(lib().mc_attn8_plan_check(_ptr(workspace), _stream(stream)), "mc_attn8_plan_check")
+
+
+def mc_prefix_prefill_attn8(pool: mc_pool8_desc, layer, q, num_q_heads, batch, total_q, cu_q, begin,
+                            page_table, cu_pages, sm_scale, out, lse, workspace, workspace_bytes,
+                            stream=None):
+    _check(_calls.attn8(pool, layer, q, num_q_heads, batch, total_q, cu_q, begin, page_table,
+                        cu_pages, sm_scale, out, lse, workspace, workspace_bytes, stream),
+           "mc_prefix_prefill_attn8")
+
+
+def mc_kv8_compress_range(pool: mc_pool_desc, pool8: mc_pool8_desc, layer_begin, layer_end, pages,
+                          n_pages, pages8, n_pages8, s0, s1, stream=None):
+    _check(_calls.compress_range(pool, pool8, layer_begin, layer_end, pages, n_pages, pages8,
+                                 n_pages8, s0, s1, stream), "mc_kv8_compress_range")
+
+
+def mc_kv8_restore_range(pool8: mc_pool8_desc, pool: mc_pool_desc, layer_begin, layer_end, pages8,
+                         n_pages8, pages, n_pages, s0, s1, stream=None):
+    _check(_calls.restore_range(pool8, pool, layer_begin, layer_end, pages8, n_pages8, pages,
+                                n_pages, s0, s1, stream), "mc_kv8_restore_range")
+
+
+def mc_kv8_pack_range(pool: mc_pool8_desc, layer_begin, layer_end, pages, n_table_pages, s0, s1,
+                      sendbuf, stream=None):
+    _check(_calls.pack_range8(pool, layer_begin, layer_end, pages, n_table_pages, s0, s1, sendbuf,
+                              stream), "mc_kv8_pack_range")
+
+
+def mc_kv8_unpack_range(pool: mc_pool8_desc, layer_begin, layer_end, pages, n_table_pages, s0, s1,
+                        sendbuf, stream=None):
+    _check(_calls.unpack_range8(pool, layer_begin, layer_end, pages, n_table_pages, s0, s1, sendbuf,
+                                stream), "mc_kv8_unpack_range")
+
+
+def mc_kv8_copy_page(pool: mc_pool8_desc, layer_begin, layer_end, src_page, dst_page, stream=None):
+    _check(_calls.copy_page8(pool, layer_begin, layer_end, src_page, dst_page, stream),
+           "mc_kv8_copy_page")

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmc_kv.so")
-SOURCES = ["mc_host.hip", "mc_copy.hip", "mc_attn.hip"]
+SOURCES = ["mc_host.hip", "mc_copy.hip", "mc_attn.hip", "mc_copy8.hip", "mc_attn8.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -1,0 +1,970 @@
+// Attention of the new token range over a paged KV cache held in 8 bits (see mc_fp8.h for the codes), for gfx950.
+//
+// Work
+//   * A q tile is 128 rows (TOK = 128 / G tokens x the G query heads of one kv head) of one sequence, or all of its
+//     rows where those are at most 16 (decode steps).  A tile walks the 64-key KV tiles that its rows may see.
+//   * All visits of KV tiles by q tiles, kv head after kv head, form one line; plan8_kernel writes down how many
+//     visits lie before each sequence, and the attention launch cuts the line into as many equal spans as
+//     workgroups run at a time.  A span is any mixture of whole q tiles and parts of some; a part's rows (O, maximum, sum)
+//     go to the workspace, and the last workgroup to finish a part of a q tile combines them, in their order.
+//   * Codes become 16-bit numbers in registers, by the instructions that convert two at a time and multiply by the
+//     block's scale (exactly: it is a power of two), and go into the 16-bit matrix instructions.
+#include <math.h>
+
+#include "mc_fp8.h"
+
+namespace {
+
+using mc::kBlockBytes;
+using mc::kHeadDim;
+using mc::kPage;
+using mc::kRowBytes;
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;     // 4 wavefronts
+constexpr int kTileRows = 128, kFewRows = 16;
+constexpr int kBN = 64;           // keys per KV tile: 4 pages
+constexpr int kSpans = 512;       // workgroups of the attention launch: two for each of 256 compute units
+constexpr int kXcds = 8;
+constexpr int kMinSpan = 4;       // visits a span has at least
+constexpr int32_t kPlanMagic = 0x6d63706d;
+
+struct Plan8Header {
+  int32_t magic;
+  int32_t heads;       // kv heads and group size of the plan, as in mc_attn.hip
+  int32_t batch;
+  int32_t total_q;
+  int64_t visits;      // of all q tiles of one kv head
+  int64_t span;        // visits per workgroup
+  int32_t pad[8];
+};
+static_assert(sizeof(Plan8Header) == 64, "header is 64 bytes");
+
+// A sequence as the plan saw it.
+struct PlanSeq {
+  int32_t begin, q_first, q, table_off;
+};
+
+struct Workspace8 {
+  size_t cum, seqs, verdict, arrivals, part_ml, part_o, total;
+  int32_t part_rows;
+};
+
+inline size_t round64(size_t x) { return (x + 63) & ~size_t(63); }
+
+// Every span has at most two parts of q tiles: the end of one that began in an earlier span (or a piece out of
+// the middle of one), and the beginning of one that goes on behind it.
+inline Workspace8 workspace8(int32_t batch, int32_t total_q, int G) {
+  Workspace8 w;
+  w.part_rows = (int64_t)total_q * G <= kFewRows ? kFewRows : kTileRows;
+  w.cum = sizeof(Plan8Header);
+  w.seqs = w.cum + round64(sizeof(int64_t) * ((size_t)batch + 1));
+  w.verdict = w.seqs + round64(sizeof(PlanSeq) * (size_t)batch);
+  w.arrivals = w.verdict + round64(sizeof(int32_t) * (size_t)batch);
+  w.part_ml = w.arrivals + round64(sizeof(uint32_t) * kSpans);
+  w.part_o = w.part_ml + sizeof(float) * 2 * 2 * kSpans * (size_t)w.part_rows;
+  w.total = w.part_o + sizeof(float) * kHeadDim * 2 * kSpans * (size_t)w.part_rows;
+  return w;
+}
+
+// ---- q tiles of a sequence -----------------------------------------------------------------
+__device__ __forceinline__ bool few_rows(int q, int G) { return (int64_t)q * G <= kFewRows; }
+template <int G>
+__device__ __forceinline__ int tile_tokens(int q) {
+  return few_rows(q, G) ? kFewRows / G : kTileRows / G;
+}
+__device__ __forceinline__ int64_t tiles64(int64_t keys) { return (keys + kBN - 1) / kBN; }
+
+// Visits of a sequence's first i q tiles, of `tok` tokens each (a power of two): tile j sees the keys before
+// b + min((j + 1) tok, q).
+__device__ __forceinline__ int64_t visits_before(int64_t b, int64_t q, int tok, int64_t i) {
+  int64_t n = i, sum = 0;
+  if (i * tok > q) {                 // the last tile is short
+    n = i - 1;
+    sum = tiles64(b + q);
+  }
+  if (tok >= kBN) {
+    const int64_t r = tok / kBN;
+    return sum + n * tiles64(b) + r * (n * (n + 1) / 2);
+  }
+  const int per = kBN / tok;         // tiles after which one more KV tile is seen
+  for (int res = 1; res <= per && res <= n; ++res) {
+    const int64_t cnt = (n - res) / per + 1;
+    sum += cnt * tiles64(b + (int64_t)res * tok) + cnt * (cnt - 1) / 2;
+  }
+  return sum;
+}
+
+struct Plan8Args {
+  const int32_t* cu_q;
+  const int32_t* begin;
+  const int32_t* page_table;
+  const int32_t* cu_pages;
+  Plan8Header* hdr;
+  int64_t* cum;
+  PlanSeq* seqs;
+  int32_t* verdict;
+  uint32_t* arrivals;
+  int32_t batch, total_q, num_pages, hkv, G, ahead;
+};
+
+// New tokens of sequence s, 0 if its offsets are malformed or its table too short.
+__device__ __forceinline__ int checked_tokens(const Plan8Args& a, int s, bool* bad) {
+  const int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], b = a.begin[s], p0 = a.cu_pages[s], p1 = a.cu_pages[s + 1];
+  *bad = q0 < 0 || q1 < q0 || q1 > a.total_q || b < 0 || p0 < 0 || p1 < p0 ||
+         (q1 > q0 && (int64_t)b + (q1 - q0) + a.ahead > ((int64_t)p1 - p0) * kPage);
+  return *bad ? 0 : q1 - q0;
+}
+
+// Workgroup 0 sums the visits; workgroup 1 + s looks at the page ids of sequence s.
+__global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x > 0) {
+    const int s = blockIdx.x - 1;
+    bool bad;
+    const int q = checked_tokens(a, s, &bad);
+    if (!bad && q > 0) {
+      const int32_t* table = a.page_table + a.cu_pages[s];
+      const int n = (int)(((int64_t)a.begin[s] + q + a.ahead + kPage - 1) / kPage);
+      for (int i = tid; i < n; i += kThreads) bad |= (unsigned)table[i] >= (unsigned)a.num_pages;
+    }
+    const int any = __syncthreads_or(bad);
+    if (tid == 0) a.verdict[s] = any ? MC_ERR_RANGE : MC_OK;
+    return;
+  }
+  for (int i = tid; i < kSpans; i += kThreads) a.arrivals[i] = 0;
+  __shared__ int64_t s_wave[kThreads / 64];
+  int64_t before = 0;
+  for (int s0 = 0; s0 < a.batch; s0 += kThreads) {
+    const int s = s0 + tid;
+    int64_t v = 0;
+    if (s < a.batch) {
+      bool bad;
+      const int q = checked_tokens(a, s, &bad);
+      if (q > 0) {
+        const int tok = (few_rows(q, a.G) ? kFewRows : kTileRows) / a.G;
+        v = visits_before(a.begin[s], q, tok, (q + tok - 1) / tok);
+      }
+      a.seqs[s] = PlanSeq{a.begin[s], a.cu_q[s], q, a.cu_pages[s]};
+    }
+    int64_t incl = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    int64_t base = before;
+    for (int w = 0; w < kThreads / 64; ++w) {
+      if (w < wave) base += s_wave[w];
+      before += s_wave[w];
+    }
+    if (s < a.batch) a.cum[s] = base + incl - v;
+    __syncthreads();
+  }
+  if (tid == 0) {
+    a.cum[a.batch] = before;
+    Plan8Header h = {};
+    h.magic = kPlanMagic;
+    h.heads = a.hkv * 16 + a.G;
+    h.batch = a.batch;
+    h.total_q = a.total_q;
+    h.visits = before;
+    h.span = max((before * a.hkv + kSpans - 1) / kSpans, (int64_t)kMinSpan);
+    *a.hdr = h;
+  }
+}
+
+// ---------------------------------------------------------------- attention --
+template <typename T> struct Num;
+template <> struct Num<_Float16> {
+  typedef f16x8 vec8;
+  static __device__ __forceinline__ f32x16 mfma32(vec8 a, vec8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(vec8 a, vec8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+  template <bool kHigh>
+  static __device__ __forceinline__ uint32_t from_codes(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, kHigh));
+  }
+  static constexpr uint32_t kOne = 0x3c00;
+};
+template <> struct Num<__bf16> {
+  typedef bf16x8 vec8;
+  static __device__ __forceinline__ f32x16 mfma32(vec8 a, vec8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma16(vec8 a, vec8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  template <bool kHigh>
+  static __device__ __forceinline__ uint32_t from_codes(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, kHigh));
+  }
+  static constexpr uint32_t kOne = 0x3f80;
+};
+// two fp32 to the 16-bit type (to nearest even), the first in the low half
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  t2 v;
+  v[0] = (T)x;
+  v[1] = (T)y;
+  return __builtin_bit_cast(uint32_t, v);
+}
+// eight codes -> eight numbers of the 16-bit type
+template <typename T>
+__device__ __forceinline__ typename Num<T>::vec8 numbers(uint32_t lo, uint32_t hi, float scale) {
+  const u32x4 v = {Num<T>::template from_codes<false>(lo, scale), Num<T>::template from_codes<true>(lo, scale),
+                   Num<T>::template from_codes<false>(hi, scale), Num<T>::template from_codes<true>(hi, scale)};
+  return __builtin_bit_cast(typename Num<T>::vec8, v);
+}
+// top bits of the bytes that are NaN codes (0x7f, 0xff)
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+struct Attn8Args {
+  const char* codes;       // of the layer
+  const float* scales;
+  const char* q;
+  char* out;
+  float* lse;
+  const int32_t* begin;
+  const int32_t* page_table;
+  const int32_t* cu_pages;
+  const Plan8Header* hdr;
+  const int64_t* cum;
+  const PlanSeq* seqs;
+  const int32_t* verdict;
+  uint32_t* arrivals;
+  float* part_ml;          // [part][row]: maximum (of the exponents, base 2), sum
+  float* part_o;           // [part][row][D], relative to the part's maximum
+  int32_t num_pages, hkv, hq, batch, total_q, part_rows;
+  float scale_log2;        // softmax scale x log2(e)
+};
+
+typedef __attribute__((address_space(3))) void* lds_void_ptr;
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(size_t)(lds_void_ptr)(p); }
+
+// Asynchronous copies from global memory into LDS: lane L's 16 (4) bytes land at lds_base + 16 (4) L.
+// As assembly so that the compiler does not wait for them before LDS reads of other buffers; they are waited for
+// by count before the barrier that publishes them.  (The s_nop: five wait states between a vector instruction that
+// writes a scalar register, which the address may come from, and a memory instruction that reads it.)
+__device__ __forceinline__ void copy16_to_lds(const char* base, uint32_t lane_off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(lane_off), "s"(base), "s"(lds_base) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4_to_lds(const void* base, uint32_t lane_off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dword %0, %1"
+               :: "v"(lane_off), "s"(base), "s"(lds_base) : "memory", "m0");
+}
+
+// What a workgroup works on: KV tiles [t0, t1) of the q tile of ntok tokens from q_first on, of kv head hk.
+struct Piece {
+  int hk, q_first, ntok, first_pos;  // first_pos: position of the first token
+  int t0, t1;
+  int table_off, last_entry;         // last entry of the page table that holds a key the tile sees
+  int kv_len;                        // keys the tile's last token sees
+};
+
+constexpr int kStages = 3;
+constexpr int kTileBytes = 4 * 2 * kBlockBytes;         // codes of a KV tile: page by page, K then V
+constexpr int kScaleBytes = 4 * 256;                    // its scales: page by page, K and V in turns (256 bytes land)
+constexpr int kStageBytes = kTileBytes + kScaleBytes;
+constexpr int kOStride = kHeadDim + 4;                  // floats between rows of O in LDS (few rows)
+constexpr int kFewBytes = 4 * kFewRows * kOStride * 4 + 4 * kFewRows * 8;
+constexpr int kLdsBytes = kStages * kStageBytes > kFewBytes ? kStages * kStageBytes : kFewBytes;
+
+// Address of a page's codes of one kv head's K; V lies hkv blocks behind
+__device__ __forceinline__ int64_t page_offset(const Attn8Args& a, int page, int hk) {
+  page = min(max(page, 0), a.num_pages - 1);            // (the plan has looked at them)
+  return ((int64_t)page * 2 * a.hkv + hk) * kBlockBytes;
+}
+
+// Where a piece's rows go: the result, or a part in the workspace.
+struct Target {
+  int part;            // < 0: out and lse
+};
+
+template <int G>
+__device__ __forceinline__ int64_t out_row(const Attn8Args& a, const Piece& p, int row) {
+  return (int64_t)(p.q_first + row / G) * a.hq + p.hk * G + row % G;
+}
+
+// ---- at most 16 rows ------------------------------------------------------------------------
+// Bound by reading the codes.  The four wavefronts take KV tiles in turns, each straight from memory into
+// registers, on v_mfma_f32_16x16x32.  Lane l, c = l % 16, g = l / 16: for S^T = K Q^T the matrix rows are keys,
+// and row m of product x is slot 4 x + m % 4 of page m / 4, so that a lane ends up with the 16 scores of page g
+// and query row c, P^T is the second product's operand as it lies, and that product's other operand, V^T, is
+// 16 contiguous bytes of page g's V block: no exchange between lanes but the maximum's.
+template <typename T, int G>
+__device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& p, const Target& to, char* lds) {
+  typedef typename Num<T>::vec8 vec8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int tok = min(c / G, p.ntok - 1);
+  const int my_pos = p.first_pos + tok;
+  const float c2 = a.scale_log2;
+  // Q^T operand: step 2 j + e of the d axis holds d = 64 j + 16 g + 8 e + [0, 8)
+  vec8 q[4];
+  {
+    const char* row = a.q + ((int64_t)(p.q_first + tok) * a.hq + p.hk * G + c % G) * kRowBytes;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      q[u] = *reinterpret_cast<const vec8*>(row + ((u >> 1) * 64 + g * 16 + (u & 1) * 8) * 2);
+  }
+  f32x4 o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+
+  u32x4 kc[8], vc[8];
+  float ks, vs;
+  const int32_t* table = a.page_table + p.table_off;
+  auto entry = [&](int t, int i) __attribute__((always_inline)) { return table[min(4 * t + i, p.last_entry)]; };
+  // K of tile t: page c / 4, slots c % 4 + 4 x
+  auto load_k = [&](int page) __attribute__((always_inline)) {
+    const char* at = a.codes + page_offset(a, page, p.hk) + (c & 3) * kHeadDim + g * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      kc[i] = *reinterpret_cast<const u32x4*>(at + (i >> 1) * 4 * kHeadDim + (i & 1) * 64);
+    ks = a.scales[((int64_t)min(max(page, 0), a.num_pages - 1) * a.hkv + p.hk) * 2];
+  };
+  auto load_v = [&](int page) __attribute__((always_inline)) {
+    const char* at = a.codes + page_offset(a, page, p.hk) + (int64_t)a.hkv * kBlockBytes + c * kPage;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vc[i] = *reinterpret_cast<const u32x4*>(at + i * 16 * kPage);
+    vs = a.scales[((int64_t)min(max(page, 0), a.num_pages - 1) * a.hkv + p.hk) * 2 + 1];
+  };
+  int t = p.t0 + wave;
+  if (t < p.t1) {
+    load_k(entry(t, c >> 2));
+    load_v(entry(t, g));
+  }
+  for (; t < p.t1; t += 4) {
+    const bool more = t + 4 < p.t1;
+    const int next_k = entry(more ? t + 4 : t, c >> 2), next_v = entry(more ? t + 4 : t, g);
+    f32x4 s[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const u32x4 w = kc[2 * x + j];
+        s[x] = Num<T>::mfma16(numbers<T>(w[0], w[1], ks), q[2 * j], s[x]);
+        s[x] = Num<T>::mfma16(numbers<T>(w[2], w[3], ks), q[2 * j + 1], s[x]);
+      }
+    }
+    if (more) load_k(next_k);
+    // lane: scores of keys 64 t + 16 g + 4 x + r
+    const int key0 = t * kBN + 16 * g;
+    const bool masked = t * kBN + kBN - 1 > p.first_pos;
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (key0 + i > my_pos) s[i >> 2][i & 3] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * c2;
+    if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
+      const float m_new = fmaxf(m, mx);
+      const float f = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    uint32_t pk[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][(2 * i) & 3], c2, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][(2 * i + 1) & 3], c2, -ref));
+      l += p0 + p1;
+      pk[i] = pack2<T>(p0, p1);
+    }
+    vec8 pt[2];
+    pt[0] = __builtin_bit_cast(vec8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+    pt[1] = __builtin_bit_cast(vec8, u32x4{pk[4], pk[5], pk[6], pk[7]});
+    if (masked) {
+      // slots behind the last key hold anything: no code of theirs counts
+      const int n = min(max(p.kv_len - key0, 0), 16);
+      uint32_t some = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int kept = min(max(n - 4 * j, 0), 4);
+          vc[i][j] &= kept == 4 ? 0xffffffffu : (1u << (8 * kept)) - 1u;
+          some |= nan_codes(vc[i][j]);
+        }
+      if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {
+        // 0 x NaN: such codes count for the rows that see their key, and for no other.  They are counted by a
+        // product of their places and the keys seen, and taken out of V.
+        vec8 seen[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int key = key0 + 8 * h + 2 * j;
+            w[j] = (key <= my_pos ? Num<T>::kOne : 0u) | (key + 1 <= my_pos ? Num<T>::kOne << 16 : 0u);
+          }
+          seen[h] = __builtin_bit_cast(vec8, w);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          u32x4 at;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t b = nan_codes(vc[i][j]) >> 7;
+            at[j] = b * 0x38u;           // the code of 1
+            vc[i][j] &= ~(b * 0xffu);
+          }
+          f32x4 n = {0.f, 0.f, 0.f, 0.f};
+          n = Num<T>::mfma16(numbers<T>(at[0], at[1], 1.f), seen[0], n);
+          n = Num<T>::mfma16(numbers<T>(at[2], at[3], 1.f), seen[1], n);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n[r] > 0.f) o[i][r] = __builtin_nanf("");
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      o[i] = Num<T>::mfma16(numbers<T>(vc[i][0], vc[i][1], vs), pt[0], o[i]);
+      o[i] = Num<T>::mfma16(numbers<T>(vc[i][2], vc[i][3], vs), pt[1], o[i]);
+    }
+    if (more) load_v(next_v);
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  // the four wavefronts' rows, through LDS
+  float* so = reinterpret_cast<float*>(lds);
+  float* sml = so + 4 * kFewRows * kOStride;
+  __syncthreads();                       // (earlier readers of the LDS are done)
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    *reinterpret_cast<f32x4*>(so + (wave * kFewRows + c) * kOStride + 16 * i + 4 * g) = o[i];
+  if (g == 0) {
+    sml[(wave * kFewRows + c) * 2] = m;
+    sml[(wave * kFewRows + c) * 2 + 1] = l;
+  }
+  __syncthreads();
+  const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8;
+  float mm = -INFINITY, ll = 0.f, acc[8];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sml[(w * kFewRows + row) * 2]);
+  const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = __builtin_amdgcn_exp2f(sml[(w * kFewRows + row) * 2] - ref);
+    ll += f * sml[(w * kFewRows + row) * 2 + 1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] += f * so[(w * kFewRows + row) * kOStride + d + j];
+  }
+  if (row >= p.ntok * G) return;
+  if (to.part >= 0) {
+    const int64_t at = (int64_t)to.part * a.part_rows + row;
+    float* po = a.part_o + at * kHeadDim + d;
+    *reinterpret_cast<f32x4*>(po) = f32x4{acc[0], acc[1], acc[2], acc[3]};
+    *reinterpret_cast<f32x4*>(po + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+    if (d == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{mm, ll};
+  } else {
+    const int64_t at = out_row<G>(a, p, row);
+    const float inv = 1.f / ll;
+    *reinterpret_cast<u32x4*>(a.out + at * kRowBytes + d * 2) =
+        u32x4{pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv),
+              pack2<T>(acc[4] * inv, acc[5] * inv), pack2<T>(acc[6] * inv, acc[7] * inv)};
+    if (d == 0) a.lse[at] = (mm + __builtin_amdgcn_logf(ll)) * 0.6931471805599453f;
+  }
+}
+
+// ---- 128 rows ---------------------------------------------------------------------------------
+// Each wavefront has 32 rows and walks all keys of the piece, on v_mfma_f32_32x32x16.  KV tiles are copied
+// as they lie into a ring of LDS buffers, and every wavefront converts what it reads.  Lane l, n = l % 32,
+// h = l / 32: matrix row i of S^T is slot (i / 8) * 4 + i % 4 of page (i / 4) % 2 of a pair, so a lane ends up with
+// the 16 scores of page h and query row n, and V^T is 16 contiguous bytes of that page.
+// K rows are 128 bytes, 8 chunks of 16; chunk c of slot s of page g lies at c ^ (s % 4 + 4 (g % 2)): any 8
+// neighbouring lanes of a K read then hit 8 different chunks, so all banks.  V reads are contiguous.
+template <typename T, int G>
+__device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, const Target& to, char* lds) {
+  typedef typename Num<T>::vec8 vec8;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  const int row = wave * 32 + n, tok = min(row / G, p.ntok - 1);
+  const bool active = wave * 32 < p.ntok * G;
+  const int my_pos = p.first_pos + tok;
+  const float c2 = a.scale_log2;
+  const uint32_t lds0 = lds_addr(lds);
+
+  // this wavefront copies page `wave` of every tile
+  const int32_t* table = a.page_table + p.table_off;
+  int ids = 0, ids_t = p.t0 - 64;        // lane i holds the page id of tile ids_t + i
+  const uint32_t lane16 = lane * 16;
+  uint32_t k_off[2];                     // where in a K block a lane's 16 bytes come from
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int slot = 8 * i + (lane >> 3);
+    k_off[i] = slot * kHeadDim + (((lane & 7) ^ ((slot & 3) | (wave & 1) << 2)) << 4);
+  }
+  auto copy_tile = [&](int t) __attribute__((always_inline)) {
+    if (t >= ids_t + 64) {
+      ids_t = t;
+      ids = table[min(4 * (t + lane) + wave, p.last_entry)];
+    }
+    const int page = min(max(__builtin_amdgcn_readlane(ids, t - ids_t), 0), a.num_pages - 1);
+    const char* k = a.codes + ((int64_t)page * 2 * a.hkv + p.hk) * kBlockBytes;
+    const char* v = k + (int64_t)a.hkv * kBlockBytes;
+    const uint32_t to_lds = lds0 + (t - p.t0) % kStages * kStageBytes + wave * 2 * kBlockBytes;
+    copy16_to_lds(k, k_off[0], to_lds);
+    copy16_to_lds(k, k_off[1], to_lds + 1024);
+    copy16_to_lds(v, lane16, to_lds + kBlockBytes);
+    copy16_to_lds(v, lane16 + 1024, to_lds + kBlockBytes + 1024);
+    copy4_to_lds(a.scales + ((int64_t)page * a.hkv + p.hk) * 2, (lane & 1) * 4,
+                 lds0 + (t - p.t0) % kStages * kStageBytes + kTileBytes + wave * 256);
+  };
+  constexpr int kCopies = 5;             // of a wavefront and tile
+
+  // Q^T operand: step 2 cc + e of the d axis holds d = 32 cc + 16 h + 8 e + [0, 8)
+  vec8 q[8];
+  {
+    const char* from = a.q + ((int64_t)(p.q_first + tok) * a.hq + p.hk * G + row % G) * kRowBytes;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      q[u] = *reinterpret_cast<const vec8*>(from + ((u >> 1) * 32 + h * 16 + (u & 1) * 8) * 2);
+  }
+  f32x16 o[4];
+  const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = zero;
+  float m = -INFINITY, l = 0.f;
+
+  __syncthreads();                       // (earlier readers of the LDS are done)
+  if (p.t0 < p.t1) copy_tile(p.t0);
+  if (p.t0 + 1 < p.t1) copy_tile(p.t0 + 1);
+  for (int t = p.t0; t < p.t1; ++t) {
+    // (a look-up of page ids in between makes the compiler wait for more: never for less)
+    if (t + 1 < p.t1)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 2 < p.t1) copy_tile(t + 2);
+    if (!active) continue;
+    const char* stage = lds + (t - p.t0) % kStages * kStageBytes;
+    const float* sc = reinterpret_cast<const float*>(stage + kTileBytes);
+    const int key0 = t * kBN;
+    const bool masked = key0 + kBN - 1 > p.first_pos;
+    f32x16 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      // A row n: slot (n / 8) * 4 + n % 4 of page 2 b + (n / 4) % 2
+      const int pg = 2 * b + ((n >> 2) & 1), slot = (n >> 3) * 4 + (n & 3);
+      const float ks = sc[pg * 64];
+      const char* from = stage + pg * 2 * kBlockBytes + slot * kHeadDim;
+      s[b] = zero;
+#pragma unroll
+      for (int cc = 0; cc < 4; ++cc) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(from + (((2 * cc + h) ^ ((slot & 3) | (pg & 1) << 2)) << 4));
+        s[b] = Num<T>::mfma32(numbers<T>(w[0], w[1], ks), q[2 * cc], s[b]);
+        s[b] = Num<T>::mfma32(numbers<T>(w[2], w[3], ks), q[2 * cc + 1], s[b]);
+      }
+    }
+    // lane: scores of keys key0 + 32 b + 16 h + r
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key0 + 32 * b + 16 * h + r > my_pos) s[b][r] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * c2;
+    if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
+      const float m_new = fmaxf(m, mx);
+      const float f = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    vec8 pt[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * e + 2 * j], c2, -ref));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * e + 2 * j + 1], c2, -ref));
+          l += p0 + p1;
+          w[j] = pack2<T>(p0, p1);
+        }
+        pt[b][e] = __builtin_bit_cast(vec8, w);
+      }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int pg = 2 * b + h;
+      const float vs = sc[pg * 64 + 1];
+      const char* from = stage + pg * 2 * kBlockBytes + kBlockBytes + n * kPage;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u32x4 w = *reinterpret_cast<const u32x4*>(from + i * 32 * kPage);
+        if (masked) {
+          const int first = key0 + 32 * b + 16 * h, valid = min(max(p.kv_len - first, 0), 16);
+          uint32_t some = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int kept = min(max(valid - 4 * j, 0), 4);
+            w[j] &= kept == 4 ? 0xffffffffu : (1u << (8 * kept)) - 1u;
+            some |= nan_codes(w[j]);
+          }
+          if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {      // (as in few_rows_piece)
+            f32x16 cnt = zero;
+            u32x4 at;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t x = nan_codes(w[j]) >> 7;
+              at[j] = x * 0x38u;
+              w[j] &= ~(x * 0xffu);
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              u32x4 seen;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int key = first + 8 * e + 2 * j;
+                seen[j] = (key <= my_pos ? Num<T>::kOne : 0u) | (key + 1 <= my_pos ? Num<T>::kOne << 16 : 0u);
+              }
+              cnt = Num<T>::mfma32(numbers<T>(at[2 * e], at[2 * e + 1], 1.f), __builtin_bit_cast(vec8, seen), cnt);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (cnt[r] > 0.f) o[i][r] = __builtin_nanf("");
+          }
+        }
+        o[i] = Num<T>::mfma32(numbers<T>(w[0], w[1], vs), pt[b][0], o[i]);
+        o[i] = Num<T>::mfma32(numbers<T>(w[2], w[3], vs), pt[b][1], o[i]);
+      }
+    }
+  }
+  l += __shfl_xor(l, 32);
+  if (row >= p.ntok * G) return;
+  // lane: d = 32 i + 8 j + 4 h + [0, 4) of its row
+  if (to.part >= 0) {
+    const int64_t at = (int64_t)to.part * a.part_rows + row;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(a.part_o + at * kHeadDim + 32 * i + 8 * j + 4 * h) =
+            f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+    if (h == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m, l};
+  } else {
+    const int64_t at = out_row<G>(a, p, row);
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<u32x2*>(a.out + at * kRowBytes + (32 * i + 8 * j + 4 * h) * 2) =
+            u32x2{pack2<T>(o[i][4 * j] * inv, o[i][4 * j + 1] * inv),
+                  pack2<T>(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
+    if (h == 0) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  }
+}
+
+// The parts of a q tile that spans w0 .. w0 + count - 1 have written, combined: 16 threads a row.
+template <typename T, int G>
+__device__ __forceinline__ void combine(const Attn8Args& a, const Piece& p, int w0, int count) {
+  for (int row = threadIdx.x >> 4; row < p.ntok * G; row += kThreads / 16) {
+    const int d = (threadIdx.x & 15) * 8;
+    float mm = -INFINITY, ll = 0.f, acc[8];
+    auto at = [&](int i) __attribute__((always_inline)) {
+      return (int64_t)(2 * (w0 + i) + (i == 0 ? 1 : 0)) * a.part_rows + row;
+    };
+    for (int i = 0; i < count; ++i) mm = fmaxf(mm, a.part_ml[at(i) * 2]);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    for (int i = 0; i < count; ++i) {
+      const float f = __builtin_amdgcn_exp2f(a.part_ml[at(i) * 2] - ref);
+      ll += f * a.part_ml[at(i) * 2 + 1];
+      const float* po = a.part_o + at(i) * kHeadDim + d;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += f * po[j];
+    }
+    const int64_t to = out_row<G>(a, p, row);
+    const float inv = 1.f / ll;
+    *reinterpret_cast<u32x4*>(a.out + to * kRowBytes + d * 2) =
+        u32x4{pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv),
+              pack2<T>(acc[4] * inv, acc[5] * inv), pack2<T>(acc[6] * inv, acc[7] * inv)};
+    if (d == 0) a.lse[to] = (mm + __builtin_amdgcn_logf(ll)) * 0.6931471805599453f;
+  }
+}
+
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
+  __shared__ int s_last;
+  const Plan8Header hdr = *a.hdr;
+  // the plan must be one of this very batch
+  if (hdr.magic != kPlanMagic || hdr.heads != a.hkv * 16 + G || hdr.batch != a.batch || hdr.total_q != a.total_q)
+    return;
+  const int64_t visits = hdr.visits, span = hdr.span;
+  // neighbouring spans, which share K and V, on one XCD (workgroups go to the XCDs in turns)
+  const int w = blockIdx.x % kXcds * (kSpans / kXcds) + blockIdx.x / kXcds;
+  int64_t at = w * span;
+  const int64_t end = min(at + span, visits * a.hkv);
+  if (at >= end) return;
+  int hk = (int)(at / visits);
+  int64_t in_head = at - hk * visits;
+  // the sequence: the last s with cum[s] <= in_head (of equal ones the last, which is not empty)
+  int s = 0;
+  {
+    const int lane = threadIdx.x & 63;
+    int cnt = a.batch;
+    while (cnt > 1) {
+      const int step = (cnt + 63) / 64, e = s + cnt, i = s + lane * step;
+      const unsigned long long le = __ballot(i < e && a.cum[i] <= in_head);
+      s += max((int)__popcll(le) - 1, 0) * step;
+      cnt = min(step, e - s);
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+  }
+  // the tile: the last i with visits_before(i) <= what is left
+  int64_t tile = 0;
+  {
+    const int64_t left = in_head - a.cum[s];
+    const int q = a.seqs[s].q, tok = tile_tokens<G>(q);
+    int64_t cnt = (q + tok - 1) / tok;
+    while (cnt > 1) {
+      const int64_t half = cnt / 2;
+      if (visits_before(a.seqs[s].begin, q, tok, tile + half) <= left) {
+        tile += half;
+        cnt -= half;
+      } else {
+        cnt = half;
+      }
+    }
+  }
+  while (at < end) {
+    const PlanSeq sq = a.seqs[s];
+    const int q0 = sq.q_first, q = sq.q, tok = tile_tokens<G>(q), b = sq.begin;
+    const int row0 = (int)tile * tok, ntok = min(tok, q - row0);
+    const int planned = (int)tiles64((int64_t)b + row0 + ntok);     // KV tiles of this q tile, by the plan
+    const int64_t tile_at = hk * visits + a.cum[s] + visits_before(b, q, tok, tile);
+    const int t0 = (int)(at - tile_at), t1 = (int)min((int64_t)planned, t0 + (end - at));
+    if (t0 < 0 || t1 <= t0) return;     // (never of a plan: a workspace written over)
+    const int now = a.begin[s];
+    Piece p;
+    p.hk = hk;
+    p.q_first = q0 + row0;
+    p.ntok = ntok;
+    p.first_pos = now + row0;
+    p.kv_len = p.first_pos + ntok;
+    const int actual = (int)tiles64(p.kv_len);           // begin may have grown since the plan
+    p.t0 = t0;
+    p.t1 = t1 == planned ? actual : min(t1, actual);
+    p.table_off = sq.table_off;
+    p.last_entry = (p.kv_len - 1) / kPage;
+    // what a table of the length that the plan saw cannot hold is not read
+    const bool ok = a.verdict[s] == MC_OK && now >= 0 && p.last_entry < a.cu_pages[s + 1] - p.table_off;
+    const bool whole = t0 == 0 && t1 == planned;
+    if (ok) {
+      Target to;
+      to.part = whole ? -1 : 2 * w + (t0 == 0 ? 1 : 0);
+      if (few_rows(q, G))
+        few_rows_piece<T, G>(a, p, to, lds);
+      else
+        tile_piece<T, G>(a, p, to, lds);
+      if (!whole) {
+        const int w0 = (int)(tile_at / span), count = (int)((tile_at + planned - 1) / span) - w0 + 1;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) s_last = atomicInc(a.arrivals + w0, count - 1) == (unsigned)(count - 1);
+        __syncthreads();
+        const bool last = s_last != 0;
+        if (last) {
+          __threadfence();
+          combine<T, G>(a, p, w0, count);
+        }
+      }
+    }
+    at += t1 - t0;
+    if ((tile + 1) * tok < q) {
+      ++tile;
+    } else {
+      tile = 0;
+      // the next sequence with new tokens, of this kv head or the next
+      const int64_t done = a.cum[s + 1];
+      if (done == visits) {
+        ++hk;
+        s = 0;
+        while (s + 1 < a.batch && a.cum[s + 1] == 0) ++s;
+      } else {
+        ++s;
+        while (s + 1 < a.batch && a.cum[s + 1] == done) ++s;
+      }
+    }
+  }
+}
+
+mc_status check_shape8(const mc_pool8_desc* pool, int32_t num_q_heads, int32_t batch, int32_t total_q, int* G_out) {
+  mc_status st = mc::check_pool8(pool);
+  if (st != MC_OK) return st;
+  if (num_q_heads <= 0 || batch < 0 || total_q < 0) return MC_ERR_INVALID;
+  if (num_q_heads % pool->num_kv_heads != 0) return MC_ERR_UNSUPPORTED;
+  const int G = num_q_heads / pool->num_kv_heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8) return MC_ERR_UNSUPPORTED;
+  *G_out = G;
+  return MC_OK;
+}
+
+template <typename T>
+mc_status launch_attn8(int G, hipStream_t hs, const Attn8Args& a) {
+  auto* kernel = G == 1   ? attn8_kernel<T, 1>
+                 : G == 2 ? attn8_kernel<T, 2>
+                 : G == 4 ? attn8_kernel<T, 4>
+                          : attn8_kernel<T, 8>;
+  hipLaunchKernelGGL(kernel, dim3(kSpans), dim3(kThreads), 0, hs, a);
+  return mc::launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mc_attn8_workspace_size(int32_t batch, int32_t total_q, int32_t num_q_heads, int32_t num_kv_heads) {
+  if (batch < 0 || total_q < 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads != 0) return 0;
+  const int G = num_q_heads / num_kv_heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8) return 0;
+  return workspace8(batch, total_q, G).total;
+}
+
+mc_status mc_attn8_plan_ahead(const mc_pool8_desc* pool, int32_t num_q_heads, int32_t batch, int32_t total_q,
+                              const int32_t* cu_q, const int32_t* begin, const int32_t* page_table,
+                              const int32_t* cu_pages, int32_t ahead_tokens, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (ahead_tokens < 0 || ahead_tokens > (1 << 20)) return MC_ERR_RANGE;
+  int G = 0;
+  const mc_status st = check_shape8(pool, num_q_heads, batch, total_q, &G);
+  if (st != MC_OK) return st;
+  if (!workspace || !mc::aligned16(workspace)) return MC_ERR_INVALID;
+  const Workspace8 w = workspace8(batch, total_q, G);
+  if (workspace_bytes < w.total) return MC_ERR_INVALID;
+  if (!cu_q || !cu_pages || (batch > 0 && (!begin || !page_table))) return MC_ERR_INVALID;
+  char* ws = static_cast<char*>(workspace);
+  Plan8Args a;
+  a.cu_q = cu_q;
+  a.begin = begin;
+  a.page_table = page_table;
+  a.cu_pages = cu_pages;
+  a.hdr = reinterpret_cast<Plan8Header*>(ws);
+  a.cum = reinterpret_cast<int64_t*>(ws + w.cum);
+  a.seqs = reinterpret_cast<PlanSeq*>(ws + w.seqs);
+  a.verdict = reinterpret_cast<int32_t*>(ws + w.verdict);
+  a.arrivals = reinterpret_cast<uint32_t*>(ws + w.arrivals);
+  a.batch = batch;
+  a.total_q = total_q;
+  a.num_pages = pool->num_pages;
+  a.hkv = pool->num_kv_heads;
+  a.G = G;
+  a.ahead = ahead_tokens;
+  hipLaunchKernelGGL(plan8_kernel, dim3(1 + (unsigned)batch), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  return mc::launch_status();
+}
+
+mc_status mc_attn8_plan_check(const void* workspace, void* stream) {
+  if (!workspace) return MC_ERR_INVALID;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  auto read = [&](void* to, size_t from, size_t bytes) {
+    return hipMemcpyAsync(to, static_cast<const char*>(workspace) + from, bytes, hipMemcpyDeviceToHost, hs) ==
+               hipSuccess &&
+           hipStreamSynchronize(hs) == hipSuccess;
+  };
+  Plan8Header h;
+  if (!read(&h, 0, sizeof(h))) return MC_ERR_HIP;
+  if (h.magic != kPlanMagic) return MC_ERR_INVALID;
+  const size_t verdicts = workspace8(h.batch, 0, 1).verdict;
+  int32_t some[1024];
+  for (int32_t s = 0; s < h.batch; s += 1024) {
+    const int32_t n = h.batch - s < 1024 ? h.batch - s : 1024;
+    if (!read(some, verdicts + sizeof(int32_t) * (size_t)s, sizeof(int32_t) * (size_t)n)) return MC_ERR_HIP;
+    for (int32_t i = 0; i < n; ++i)
+      if (some[i] != MC_OK) return static_cast<mc_status>(some[i]);
+  }
+  return MC_OK;
+}
+
+mc_status mc_attn8_plan(const mc_pool8_desc* pool, int32_t num_q_heads, int32_t batch, int32_t total_q,
+                        const int32_t* cu_q, const int32_t* begin, const int32_t* page_table,
+                        const int32_t* cu_pages, void* workspace, size_t workspace_bytes, void* stream) {
+  return mc_attn8_plan_ahead(pool, num_q_heads, batch, total_q, cu_q, begin, page_table, cu_pages, 0, workspace,
+                             workspace_bytes, stream);
+}
+
+mc_status mc_prefix_prefill_attn8(const mc_pool8_desc* pool, int32_t layer, const void* q, int32_t num_q_heads,
+                                  int32_t batch, int32_t total_q, const int32_t* cu_q, const int32_t* begin,
+                                  const int32_t* page_table, const int32_t* cu_pages, float sm_scale, void* out,
+                                  float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  int G = 0;
+  const mc_status st = check_shape8(pool, num_q_heads, batch, total_q, &G);
+  if (st != MC_OK) return st;
+  if (layer < 0 || layer >= pool->num_layers) return MC_ERR_RANGE;
+  if (!(sm_scale >= 0.f) || !isfinite(sm_scale)) return MC_ERR_INVALID;
+  if (batch == 0 || total_q == 0) return MC_OK;
+  if (!q || !out || !lse || !cu_q || !begin || !page_table || !cu_pages || !workspace) return MC_ERR_INVALID;
+  if (!mc::aligned16(q) || !mc::aligned16(out) || !mc::aligned16(workspace) ||
+      (reinterpret_cast<uintptr_t>(lse) & 3u))
+    return MC_ERR_INVALID;
+  const Workspace8 w = workspace8(batch, total_q, G);
+  if (workspace_bytes < w.total) return MC_ERR_INVALID;
+  char* ws = static_cast<char*>(workspace);
+  Attn8Args a;
+  a.codes = static_cast<const char*>(pool->codes) + layer * mc::layer8_stride(pool);
+  a.scales = pool->scales + layer * mc::layer8_scales(pool);
+  a.q = static_cast<const char*>(q);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.begin = begin;
+  a.page_table = page_table;
+  a.cu_pages = cu_pages;
+  a.hdr = reinterpret_cast<const Plan8Header*>(ws);
+  a.cum = reinterpret_cast<const int64_t*>(ws + w.cum);
+  a.seqs = reinterpret_cast<const PlanSeq*>(ws + w.seqs);
+  a.verdict = reinterpret_cast<const int32_t*>(ws + w.verdict);
+  a.arrivals = reinterpret_cast<uint32_t*>(ws + w.arrivals);
+  a.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
+  a.part_o = reinterpret_cast<float*>(ws + w.part_o);
+  a.num_pages = pool->num_pages;
+  a.hkv = pool->num_kv_heads;
+  a.hq = num_q_heads;
+  a.batch = batch;
+  a.total_q = total_q;
+  a.part_rows = w.part_rows;
+  const float scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)kHeadDim);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  return pool->dtype == MC_F16 ? launch_attn8<_Float16>(G, hs, a) : launch_attn8<__bf16>(G, hs, a);
+}
+
+}  // extern "C"

@@ -36,6 +36,7 @@ PyObject* s_value;
 PyObject* s_as_parameter;
 // from binding.py (setup): the types whose content is taken over, and the error for other objects
 PyObject *t_pool, *t_pointer, *t_i32, *t_size, *t_error;
+PyObject* t_pool8;
 PyObject* g_get_device;    // torch's current-device and current-stream look-ups
 PyObject* g_get_stream;
 
@@ -140,13 +141,21 @@ bool to_ptr(PyObject* o, void** out) {
   return v.p && to_handle(v.p, out);
 }
 
-// pool descriptor: the ctypes structure's own bytes
-bool to_pool(PyObject* o, mc_pool_desc* out) {
-  if (!is_a(o, t_pool)) return wrong_type(o, "an mc_pool_desc");
+// pool descriptors: the ctypes structure's own bytes
+template <typename Desc>
+bool to_desc(PyObject* o, Desc* out) {
   const Buffer v(o, PyBUF_SIMPLE);
-  if (!v.held || v.b.len < (Py_ssize_t)sizeof(mc_pool_desc)) return false;
-  memcpy(out, v.b.buf, sizeof(mc_pool_desc));
+  if (!v.held || v.b.len < (Py_ssize_t)sizeof(Desc)) return false;
+  memcpy(out, v.b.buf, sizeof(Desc));
   return true;
+}
+
+bool to_pool(PyObject* o, mc_pool_desc* out) {
+  return is_a(o, t_pool) ? to_desc(o, out) : wrong_type(o, "an mc_pool_desc");
+}
+
+bool to_pool8(PyObject* o, mc_pool8_desc* out) {
+  return is_a(o, t_pool8) ? to_desc(o, out) : wrong_type(o, "an mc_pool8_desc");
 }
 
 // stream: None = torch's current stream, an integer handle, or an object with cuda_stream
@@ -259,6 +268,7 @@ struct Args {
   void* handle() { return get<void*>(to_handle); }
   void* stream() { return get<void*>(to_stream); }
   mc_pool_desc pool() { return get<mc_pool_desc>(to_pool); }
+  mc_pool8_desc pool8() { return get<mc_pool8_desc>(to_pool8); }
   std::vector<int32_t> list() { return get<std::vector<int32_t>>(to_list); }
   const int32_t* pi32() { return static_cast<const int32_t*>(ptr()); }
   float f32() {
@@ -390,6 +400,103 @@ PyObject* copy_page(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* stream = g.stream();
   if (!g.ok) return nullptr;
   CALL(mc_kv_copy_page(&pool, l0, l1, src, dst, slots, stream));
+}
+
+// ---- device calls of the cache in 8 bits ----
+PyObject* append8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 11);
+  const mc_pool8_desc pool = g.pool8();
+  const int32_t layer = g.i32();
+  const void *k = g.ptr(), *v = g.ptr();
+  const int32_t batch = g.i32(), tq = g.i32();
+  const int32_t *cu_q = g.pi32(), *begin = g.pi32(), *table = g.pi32(), *cu_pages = g.pi32();
+  void* stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(mc_kv8_append(&pool, layer, k, v, batch, tq, cu_q, begin, table, cu_pages, stream));
+}
+
+// plan8(pool, hq, batch, total_q, cu_q, begin, table, cu_pages, ahead, ws, ws_bytes, stream)
+PyObject* plan8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 12);
+  const mc_pool8_desc pool = g.pool8();
+  const int32_t hq = g.i32(), batch = g.i32(), tq = g.i32();
+  const int32_t *cu_q = g.pi32(), *begin = g.pi32(), *table = g.pi32(), *cu_pages = g.pi32();
+  const int32_t ahead = g.i32();
+  void* ws = g.ptr();
+  const size_t bytes = g.size();
+  void* stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(mc_attn8_plan_ahead(&pool, hq, batch, tq, cu_q, begin, table, cu_pages, ahead, ws, bytes,
+                           stream));
+}
+
+PyObject* attn8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 16);
+  const mc_pool8_desc pool = g.pool8();
+  const int32_t layer = g.i32();
+  const void* q = g.ptr();
+  const int32_t hq = g.i32(), batch = g.i32(), tq = g.i32();
+  const int32_t *cu_q = g.pi32(), *begin = g.pi32(), *table = g.pi32(), *cu_pages = g.pi32();
+  const float scale = g.f32();
+  void* out = g.ptr();
+  float* lse = static_cast<float*>(g.ptr());
+  void* ws = g.ptr();
+  const size_t bytes = g.size();
+  void* stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(mc_prefix_prefill_attn8(&pool, layer, q, hq, batch, tq, cu_q, begin, table, cu_pages, scale,
+                               out, lse, ws, bytes, stream));
+}
+
+// the pool read, the pool written, layers, their tables in that order, range, stream
+PyObject* compress_range(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 11);
+  const mc_pool_desc pool = g.pool();
+  const mc_pool8_desc pool8 = g.pool8();
+  const int32_t l0 = g.i32(), l1 = g.i32();
+  const int32_t* pages = g.pi32();
+  const int32_t n_pages = g.i32();
+  const int32_t* pages8 = g.pi32();
+  const int32_t n_pages8 = g.i32(), s0 = g.i32(), s1 = g.i32();
+  void* stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(mc_kv8_compress_range(&pool, &pool8, l0, l1, pages, n_pages, pages8, n_pages8, s0, s1, stream));
+}
+
+PyObject* restore_range(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 11);
+  const mc_pool8_desc pool8 = g.pool8();
+  const mc_pool_desc pool = g.pool();
+  const int32_t l0 = g.i32(), l1 = g.i32();
+  const int32_t* pages8 = g.pi32();
+  const int32_t n_pages8 = g.i32();
+  const int32_t* pages = g.pi32();
+  const int32_t n_pages = g.i32(), s0 = g.i32(), s1 = g.i32();
+  void* stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(mc_kv8_restore_range(&pool8, &pool, l0, l1, pages8, n_pages8, pages, n_pages, s0, s1, stream));
+}
+
+template <bool kPack>
+PyObject* copy_range8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 9);
+  const mc_pool8_desc pool = g.pool8();
+  const int32_t l0 = g.i32(), l1 = g.i32();
+  const int32_t* pages = g.pi32();
+  const int32_t n_pages = g.i32(), s0 = g.i32(), s1 = g.i32();
+  void *buf = g.ptr(), *stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(kPack ? mc_kv8_pack_range(&pool, l0, l1, pages, n_pages, s0, s1, buf, stream)
+             : mc_kv8_unpack_range(&pool, l0, l1, pages, n_pages, s0, s1, buf, stream));
+}
+
+PyObject* copy_page8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args g(a, n, 6);
+  const mc_pool8_desc pool = g.pool8();
+  const int32_t l0 = g.i32(), l1 = g.i32(), src = g.i32(), dst = g.i32();
+  void* stream = g.stream();
+  if (!g.ok) return nullptr;
+  CALL(mc_kv8_copy_page(&pool, l0, l1, src, dst, stream));
 }
 
 // ---- host calls ----
@@ -570,12 +677,22 @@ PyObject* setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// setup8(mc_pool8_desc)
+PyObject* setup8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 1 || !PyType_Check(a[0])) return PyErr_Format(PyExc_TypeError, "one type is expected");
+  Py_INCREF(a[0]);
+  Py_XSETREF(t_pool8, a[0]);
+  Py_RETURN_NONE;
+}
+
 #define ENTRY(name, fn) {name, (PyCFunction)(void (*)(void))guarded<fn>, METH_FASTCALL, nullptr}
 #define FN(fn) ENTRY(#fn, fn)
 PyMethodDef kMethods[] = {
     FN(setup), FN(append), FN(append_send), FN(plan), FN(attn), FN(attn_noalloc), FN(copy_page),
     ENTRY("pack_range", copy_range<true>), ENTRY("unpack_range", copy_range<false>),
     ENTRY("pack_batch", copy_batch<true>), ENTRY("unpack_batch", copy_batch<false>),
+    FN(setup8), FN(append8), FN(plan8), FN(attn8), FN(compress_range), FN(restore_range),
+    ENTRY("pack_range8", copy_range8<true>), ENTRY("unpack_range8", copy_range8<false>), FN(copy_page8),
     FN(alloc_pages), FN(free_pages), FN(check_page_table), FN(plan_remote_send),
     FN(addr_compress), FN(addr_expand), FN(index_insert), FN(index_match), FN(prep_recv),
     {nullptr, nullptr, 0, nullptr}};
