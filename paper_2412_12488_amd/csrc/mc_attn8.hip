@@ -11,6 +11,8 @@
 //     block's scale (exactly: it is a power of two), and go into the 16-bit matrix instructions.
 #include <math.h>
 
+#include <type_traits>
+
 #include "mc_fp8.h"
 
 namespace {
@@ -47,13 +49,18 @@ struct Plan8Header {
 };
 static_assert(sizeof(Plan8Header) == 64, "header is 64 bytes");
 
+// A q tile of more than 16 rows that the spans from one on cut: which merge8_kernel combines.
+struct MergeRec8 {
+  int32_t q_first, ntok, hk, count;   // count: its parts, 0: none
+};
+
 // A sequence as the plan saw it.
 struct PlanSeq {
   int32_t begin, q_first, q, table_off;
 };
 
 struct Workspace8 {
-  size_t cum, seqs, verdict, arrivals, part_ml, part_o, total;
+  size_t cum, seqs, verdict, arrivals, merges, part_ml, part_o, total;
   int32_t part_rows;
 };
 
@@ -68,7 +75,8 @@ inline Workspace8 workspace8(int32_t batch, int32_t total_q, int G) {
   w.seqs = w.cum + round64(sizeof(int64_t) * ((size_t)batch + 1));
   w.verdict = w.seqs + round64(sizeof(PlanSeq) * (size_t)batch);
   w.arrivals = w.verdict + round64(sizeof(int32_t) * (size_t)batch);
-  w.part_ml = w.arrivals + round64(sizeof(uint32_t) * kSpans);
+  w.merges = w.arrivals + round64(sizeof(uint32_t) * kSpans);
+  w.part_ml = w.merges + sizeof(MergeRec8) * kSpans;
   w.part_o = w.part_ml + sizeof(float) * 2 * 2 * kSpans * (size_t)w.part_rows;
   w.total = w.part_o + sizeof(float) * kHeadDim * 2 * kSpans * (size_t)w.part_rows;
   return w;
@@ -246,9 +254,11 @@ struct Attn8Args {
   const PlanSeq* seqs;
   const int32_t* verdict;
   uint32_t* arrivals;
+  MergeRec8* merges;
   float* part_ml;          // [part][row]: maximum (of the exponents, base 2), sum
   float* part_o;           // [part][row][D], relative to the part's maximum
   int32_t num_pages, hkv, hq, batch, total_q, part_rows;
+  int32_t behind;          // whether cut q tiles of more than 16 rows are left to merge8_kernel
   float scale_log2;        // softmax scale x log2(e)
 };
 
@@ -293,6 +303,41 @@ __device__ __forceinline__ int64_t page_offset(const Attn8Args& a, int page, int
 // Where a piece's rows go: the result, or a part in the workspace.
 struct Target {
   int part;            // < 0: out and lse
+};
+
+// Parts of a q tile are written by one workgroup and read by another of the same launch, on any XCD: through
+// buffer instructions of device scope (sc1), which go to the level that all XCDs share, so that no L2 has to be
+// written back or invalidated as a whole (with fences of device scope instead, 256 decode rows took 485 us a
+// layer).  What merge8_kernel reads goes by plain ones.
+typedef __amdgpu_buffer_rsrc_t buffer_rsrc;
+constexpr int kDeviceScope = 16, kLaunchScope = 0;
+__device__ __forceinline__ buffer_rsrc make_rsrc(void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, 0, (uint32_t)bytes, 0x00020000);   // raw, 32-bit; bounds checked
+}
+struct Parts {
+  buffer_rsrc o, ml;
+  int rows;
+  __device__ __forceinline__ explicit Parts(const Attn8Args& a)
+      : o(make_rsrc(a.part_o, 2ll * kSpans * a.part_rows * kHeadDim * 4)),
+        ml(make_rsrc(a.part_ml, 2ll * kSpans * a.part_rows * 8)), rows(a.part_rows) {}
+  __device__ __forceinline__ uint32_t at(int part, int row) const { return (uint32_t)(part * rows + row); }
+  template <int kScope>
+  __device__ __forceinline__ void put(uint32_t i, int d, f32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), o, (i * kHeadDim + d) * 4, 0, kScope);
+  }
+  template <int kScope>
+  __device__ __forceinline__ void put_ml(uint32_t i, float m, float l) const {
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, l)}, ml,
+                                          i * 8, 0, kScope);
+  }
+  template <int kScope>
+  __device__ __forceinline__ f32x4 get(uint32_t i, int d) const {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(o, (i * kHeadDim + d) * 4, 0, kScope));
+  }
+  template <int kScope>
+  __device__ __forceinline__ f32x2 get_ml(uint32_t i) const {
+    return __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(ml, i * 8, 0, kScope));
+  }
 };
 
 template <int G>
@@ -478,11 +523,11 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
   }
   if (row >= p.ntok * G) return;
   if (to.part >= 0) {
-    const int64_t at = (int64_t)to.part * a.part_rows + row;
-    float* po = a.part_o + at * kHeadDim + d;
-    *reinterpret_cast<f32x4*>(po) = f32x4{acc[0], acc[1], acc[2], acc[3]};
-    *reinterpret_cast<f32x4*>(po + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
-    if (d == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{mm, ll};
+    const Parts parts(a);
+    const uint32_t at = parts.at(to.part, row);
+    parts.put<kDeviceScope>(at, d, f32x4{acc[0], acc[1], acc[2], acc[3]});
+    parts.put<kDeviceScope>(at, d + 4, f32x4{acc[4], acc[5], acc[6], acc[7]});
+    if (d == 0) parts.put_ml<kDeviceScope>(at, mm, ll);
   } else {
     const int64_t at = out_row<G>(a, p, row);
     const float inv = 1.f / ll;
@@ -670,14 +715,22 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   if (row >= p.ntok * G) return;
   // lane: d = 32 i + 8 j + 4 h + [0, 4) of its row
   if (to.part >= 0) {
-    const int64_t at = (int64_t)to.part * a.part_rows + row;
+    const Parts parts(a);
+    const uint32_t at = parts.at(to.part, row);
+    auto store = [&](auto scope) __attribute__((always_inline)) {
+      constexpr int kScope = decltype(scope)::value;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4*>(a.part_o + at * kHeadDim + 32 * i + 8 * j + 4 * h) =
-            f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-    if (h == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{m, l};
+        for (int j = 0; j < 4; ++j)
+          parts.put<kScope>(at, 32 * i + 8 * j + 4 * h,
+                            f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
+      if (h == 0) parts.put_ml<kScope>(at, m, l);
+    };
+    if (a.behind)
+      store(std::integral_constant<int, kLaunchScope>());
+    else
+      store(std::integral_constant<int, kDeviceScope>());
   } else {
     const int64_t at = out_row<G>(a, p, row);
     const float inv = 1.f / l;
@@ -692,33 +745,71 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   }
 }
 
-// The parts of a q tile that spans w0 .. w0 + count - 1 have written, combined: 16 threads a row.
-template <typename T, int G>
-__device__ __forceinline__ void combine(const Attn8Args& a, const Piece& p, int w0, int count) {
-  for (int row = threadIdx.x >> 4; row < p.ntok * G; row += kThreads / 16) {
-    const int d = (threadIdx.x & 15) * 8;
-    float mm = -INFINITY, ll = 0.f, acc[8];
+// Rows first, first + step .. of a q tile whose parts spans w0 .. w0 + count - 1 have written, combined in their order:
+// 16 threads a row.  kAhead parts are requested at a time.
+template <typename T, int G, int kScope, int kAhead>
+__device__ __forceinline__ void combine(const Attn8Args& a, const Piece& p, int w0, int count, int first, int step) {
+  const Parts parts(a);
+  const int d = (threadIdx.x & 15) * 8;
+  for (int row = first + (threadIdx.x >> 4); row < p.ntok * G; row += step) {
+    // part 0 is the tile's beginning, at the end of its span; the others lie at the beginning of theirs
     auto at = [&](int i) __attribute__((always_inline)) {
-      return (int64_t)(2 * (w0 + i) + (i == 0 ? 1 : 0)) * a.part_rows + row;
+      i = min(i, count - 1);
+      return parts.at(2 * (w0 + i) + (i == 0 ? 1 : 0), row);
     };
-    for (int i = 0; i < count; ++i) mm = fmaxf(mm, a.part_ml[at(i) * 2]);
-    const float ref = mm == -INFINITY ? 0.f : mm;
+    float m = -INFINITY, l = 0.f;
+    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+      f32x2 ml[kAhead];
+      f32x4 o[kAhead][2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    for (int i = 0; i < count; ++i) {
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[at(i) * 2] - ref);
-      ll += f * a.part_ml[at(i) * 2 + 1];
-      const float* po = a.part_o + at(i) * kHeadDim + d;
+      for (int i = 0; i < kAhead; ++i) ml[i] = parts.get_ml<kScope>(at(i0 + i));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += f * po[j];
+      for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) o[i][j] = parts.get<kScope>(at(i0 + i), d + 4 * j);
+      float mx = m;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) mx = fmaxf(mx, ml[i][0]);
+      const float ref = mx == -INFINITY ? 0.f : mx, f0 = __builtin_amdgcn_exp2f(m - ref);
+      l *= f0;
+      acc[0] *= f0;
+      acc[1] *= f0;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const float f = i0 + i < count ? __builtin_amdgcn_exp2f(ml[i][0] - ref) : 0.f;
+        if (i0 + i < count) {
+          l += f * ml[i][1];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[j] += f * o[i][j];
+        }
+      }
+      m = mx;
     }
     const int64_t to = out_row<G>(a, p, row);
-    const float inv = 1.f / ll;
+    const float inv = 1.f / l;
     *reinterpret_cast<u32x4*>(a.out + to * kRowBytes + d * 2) =
-        u32x4{pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv),
-              pack2<T>(acc[4] * inv, acc[5] * inv), pack2<T>(acc[6] * inv, acc[7] * inv)};
-    if (d == 0) a.lse[to] = (mm + __builtin_amdgcn_logf(ll)) * 0.6931471805599453f;
+        u32x4{pack2<T>(acc[0][0] * inv, acc[0][1] * inv), pack2<T>(acc[0][2] * inv, acc[0][3] * inv),
+              pack2<T>(acc[1][0] * inv, acc[1][1] * inv), pack2<T>(acc[1][2] * inv, acc[1][3] * inv)};
+    if (d == 0) a.lse[to] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
+}
+
+// Cut q tiles of more than 16 rows, in a launch of its own: workgroup (span of a tile's beginning, 16 rows in turns).
+constexpr int kMergeBlocks = 4;
+template <typename T, int G>
+__global__ __launch_bounds__(kThreads) void merge8_kernel(Attn8Args a) {
+  const Plan8Header hdr = *a.hdr;
+  if (hdr.magic != kPlanMagic || hdr.heads != a.hkv * 16 + G || hdr.batch != a.batch || hdr.total_q != a.total_q)
+    return;
+  const int w = blockIdx.x / kMergeBlocks;
+  const MergeRec8 r = a.merges[w];
+  if (r.count < 2 || w + r.count > kSpans) return;
+  Piece p = {};
+  p.hk = r.hk;
+  p.q_first = r.q_first;
+  p.ntok = r.ntok;
+  combine<T, G, kLaunchScope, 4>(a, p, w, r.count, blockIdx.x % kMergeBlocks * 16, 16 * kMergeBlocks);
 }
 
 template <typename T, int G>
@@ -732,6 +823,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   const int64_t visits = hdr.visits, span = hdr.span;
   // neighbouring spans, which share K and V, on one XCD (workgroups go to the XCDs in turns)
   const int w = blockIdx.x % kXcds * (kSpans / kXcds) + blockIdx.x / kXcds;
+  if (a.behind && threadIdx.x == 0) a.merges[w].count = 0;
   int64_t at = w * span;
   const int64_t end = min(at + span, visits * a.hkv);
   if (at >= end) return;
@@ -798,14 +890,20 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
         tile_piece<T, G>(a, p, to, lds);
       if (!whole) {
         const int w0 = (int)(tile_at / span), count = (int)((tile_at + planned - 1) / span) - w0 + 1;
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) s_last = atomicInc(a.arrivals + w0, count - 1) == (unsigned)(count - 1);
-        __syncthreads();
-        const bool last = s_last != 0;
-        if (last) {
-          __threadfence();
-          combine<T, G>(a, p, w0, count);
+        if (a.behind && !few_rows(q, G)) {
+          if (t0 == 0 && threadIdx.x == 0) a.merges[w] = MergeRec8{p.q_first, p.ntok, p.hk, count};
+        } else {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wavefront's rows have been written
+          __syncthreads();
+          if (threadIdx.x == 0)
+            s_last = __hip_atomic_fetch_add(a.arrivals + w0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                     (unsigned)(count - 1);
+          __syncthreads();
+          if (s_last) {
+            if (threadIdx.x == 0)      // for the next layer
+              __hip_atomic_store(a.arrivals + w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            combine<T, G, kDeviceScope, 8>(a, p, w0, count, 0, kThreads / 16);
+          }
         }
       }
     }
@@ -846,6 +944,13 @@ mc_status launch_attn8(int G, hipStream_t hs, const Attn8Args& a) {
                  : G == 4 ? attn8_kernel<T, 4>
                           : attn8_kernel<T, 8>;
   hipLaunchKernelGGL(kernel, dim3(kSpans), dim3(kThreads), 0, hs, a);
+  mc_status st = mc::launch_status();
+  if (st != MC_OK || !a.behind) return st;
+  auto* merge = G == 1   ? merge8_kernel<T, 1>
+                : G == 2 ? merge8_kernel<T, 2>
+                : G == 4 ? merge8_kernel<T, 4>
+                         : merge8_kernel<T, 8>;
+  hipLaunchKernelGGL(merge, dim3(kSpans * kMergeBlocks), dim3(kThreads), 0, hs, a);
   return mc::launch_status();
 }
 
@@ -953,6 +1058,7 @@ mc_status mc_prefix_prefill_attn8(const mc_pool8_desc* pool, int32_t layer, cons
   a.seqs = reinterpret_cast<const PlanSeq*>(ws + w.seqs);
   a.verdict = reinterpret_cast<const int32_t*>(ws + w.verdict);
   a.arrivals = reinterpret_cast<uint32_t*>(ws + w.arrivals);
+  a.merges = reinterpret_cast<MergeRec8*>(ws + w.merges);
   a.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + w.part_o);
   a.num_pages = pool->num_pages;
@@ -961,6 +1067,8 @@ mc_status mc_prefix_prefill_attn8(const mc_pool8_desc* pool, int32_t layer, cons
   a.batch = batch;
   a.total_q = total_q;
   a.part_rows = w.part_rows;
+  // (more than one new token for a sequence on average: some may be q tiles of many rows)
+  a.behind = total_q > batch && (int64_t)total_q * G > kFewRows;
   const float scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)kHeadDim);
   a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t hs = static_cast<hipStream_t>(stream);
