@@ -33,7 +33,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;     // 4 wavefronts
 constexpr int kTileRows = 128, kFewRows = 16;
 constexpr int kBN = 64;           // keys per KV tile: 4 pages
-constexpr int kSpans = 512;       // workgroups of the attention launch: two for each of 256 compute units
+constexpr int kSpans = 512;       // workgroups of an attention launch at most: two for each of 256 compute units
 constexpr int kXcds = 8;
 constexpr int kMinSpan = 4;       // visits a span has at least
 constexpr int32_t kPlanMagic = 0x6d63706d;
@@ -45,7 +45,8 @@ struct Plan8Header {
   int32_t total_q;
   int64_t visits;      // of all q tiles of one kv head
   int64_t span;        // visits per workgroup
-  int32_t pad[8];
+  int32_t tile_rows;   // rows of a q tile at most: kTileRows, or kFewRows
+  int32_t pad[7];
 };
 static_assert(sizeof(Plan8Header) == 64, "header is 64 bytes");
 
@@ -61,32 +62,40 @@ struct PlanSeq {
 
 struct Workspace8 {
   size_t cum, seqs, verdict, arrivals, merges, part_ml, part_o, total;
-  int32_t part_rows;
+  int32_t part_rows, spans;
+  bool few;
 };
 
+inline bool few_rows_only(int32_t batch, int32_t total_q, int G);
 inline size_t round64(size_t x) { return (x + 63) & ~size_t(63); }
 
 // Every span has at most two parts of q tiles: the end of one that began in an earlier span (or a piece out of
 // the middle of one), and the beginning of one that goes on behind it.
 inline Workspace8 workspace8(int32_t batch, int32_t total_q, int G) {
   Workspace8 w;
-  w.part_rows = (int64_t)total_q * G <= kFewRows ? kFewRows : kTileRows;
+  w.few = few_rows_only(batch, total_q, G);
+  w.spans = kSpans;
+  w.part_rows = w.few ? kFewRows : kTileRows;
   w.cum = sizeof(Plan8Header);
   w.seqs = w.cum + round64(sizeof(int64_t) * ((size_t)batch + 1));
   w.verdict = w.seqs + round64(sizeof(PlanSeq) * (size_t)batch);
   w.arrivals = w.verdict + round64(sizeof(int32_t) * (size_t)batch);
   w.merges = w.arrivals + round64(sizeof(uint32_t) * kSpans);
   w.part_ml = w.merges + sizeof(MergeRec8) * kSpans;
-  w.part_o = w.part_ml + sizeof(float) * 2 * 2 * kSpans * (size_t)w.part_rows;
-  w.total = w.part_o + sizeof(float) * kHeadDim * 2 * kSpans * (size_t)w.part_rows;
+  w.part_o = w.part_ml + sizeof(float) * 2 * 2 * (size_t)w.spans * w.part_rows;
+  w.total = w.part_o + sizeof(float) * kHeadDim * 2 * (size_t)w.spans * w.part_rows;
   return w;
 }
 
 // ---- q tiles of a sequence -----------------------------------------------------------------
-__device__ __forceinline__ bool few_rows(int q, int G) { return (int64_t)q * G <= kFewRows; }
-template <int G>
-__device__ __forceinline__ int tile_tokens(int q) {
-  return few_rows(q, G) ? kFewRows / G : kTileRows / G;
+// Two kinds of plan, by the batch's sizes alone.  Batches of no more new tokens than sequences (decode steps) have
+// q tiles of at most 16 rows, whatever the sequences have, and a kernel that knows no others.  In other batches sequences
+// of at most 16 rows have one such tile and others tiles of 128 rows.
+inline bool few_rows_only(int32_t batch, int32_t total_q, int G) {
+  return total_q <= batch || (int64_t)total_q * G <= kFewRows;
+}
+__device__ __forceinline__ int rows_of_tiles(int q, int G, int tile_rows) {
+  return (int64_t)q * G <= kFewRows ? kFewRows : tile_rows;
 }
 __device__ __forceinline__ int64_t tiles64(int64_t keys) { return (keys + kBN - 1) / kBN; }
 
@@ -121,6 +130,7 @@ struct Plan8Args {
   int32_t* verdict;
   uint32_t* arrivals;
   int32_t batch, total_q, num_pages, hkv, G, ahead;
+  int32_t tile_rows, spans;
 };
 
 // New tokens of sequence s, 0 if its offsets are malformed or its table too short.
@@ -157,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
       bool bad;
       const int q = checked_tokens(a, s, &bad);
       if (q > 0) {
-        const int tok = (few_rows(q, a.G) ? kFewRows : kTileRows) / a.G;
+        const int tok = rows_of_tiles(q, a.G, a.tile_rows) / a.G;
         v = visits_before(a.begin[s], q, tok, (q + tok - 1) / tok);
       }
       a.seqs[s] = PlanSeq{a.begin[s], a.cu_q[s], q, a.cu_pages[s]};
@@ -186,7 +196,8 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
     h.batch = a.batch;
     h.total_q = a.total_q;
     h.visits = before;
-    h.span = max((before * a.hkv + kSpans - 1) / kSpans, (int64_t)kMinSpan);
+    h.span = max((before * a.hkv + a.spans - 1) / a.spans, (int64_t)kMinSpan);
+    h.tile_rows = a.tile_rows;
     *a.hdr = h;
   }
 }
@@ -205,7 +216,6 @@ template <> struct Num<_Float16> {
   static __device__ __forceinline__ uint32_t from_codes(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, kHigh));
   }
-  static constexpr uint32_t kOne = 0x3c00;
 };
 template <> struct Num<__bf16> {
   typedef bf16x8 vec8;
@@ -219,7 +229,6 @@ template <> struct Num<__bf16> {
   static __device__ __forceinline__ uint32_t from_codes(uint32_t w, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, kHigh));
   }
-  static constexpr uint32_t kOne = 0x3f80;
 };
 // two fp32 to the 16-bit type (to nearest even), the first in the low half
 template <typename T>
@@ -237,8 +246,45 @@ __device__ __forceinline__ typename Num<T>::vec8 numbers(uint32_t lo, uint32_t h
                    Num<T>::template from_codes<false>(hi, scale), Num<T>::template from_codes<true>(hi, scale)};
   return __builtin_bit_cast(typename Num<T>::vec8, v);
 }
+// The largest of three, a NaN if one is, in one instruction (fmaxf quiets each operand by another).  What follows from a
+// NaN maximum: the reference stays, and the row's sum is a NaN anyway.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+// x's upper 32 lanes <-> y's lower 32 lanes.  (The builtin of this hands out its first result twice where both operands are
+// one value; the s_nop is the distance to the vector instructions that wrote them.)
+__device__ __forceinline__ void swap_halves(uint32_t& x, uint32_t& y) {
+  asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(x), "+v"(y));
+}
 // top bits of the bytes that are NaN codes (0x7f, 0xff)
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+// A NaN in V counts for the rows that see its key, and for no other, but P is 0 for those and 0 x NaN is NaN.  So in
+// KV tiles that not all rows see whole, NaN codes are taken out of V, and their places, as 2^126, go through a product
+// with the keys that each row sees, as 2^126 or 0: that adds an infinity where both are, and a second
+// one of the other sign makes it a NaN.  (In bf16, whatever the pool's type: fp16 has no such numbers.)
+__device__ __forceinline__ u32x4 take_nan_codes(u32x4& v) {
+  u32x4 at;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t b = nan_codes(v[j]) >> 7;
+    at[j] = b * 0x38u;                   // the code of 1
+    v[j] &= ~(b * 0xffu);
+  }
+  return at;
+}
+__device__ __forceinline__ bf16x8 huge(u32x4 at, int half, bool positive) {
+  u32x4 w = __builtin_bit_cast(u32x4, numbers<__bf16>(at[2 * half], at[2 * half + 1], 0x1p126f));
+  if (!positive) w ^= 0x80008000u;
+  return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ bf16x8 keys_seen(int key, int pos) {
+  u32x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j] = (key + 2 * j <= pos ? 0x7e80u : 0u) | (key + 2 * j + 1 <= pos ? 0x7e800000u : 0u);
+  return __builtin_bit_cast(bf16x8, w);
+}
 
 struct Attn8Args {
   const char* codes;       // of the layer
@@ -258,7 +304,7 @@ struct Attn8Args {
   float* part_ml;          // [part][row]: maximum (of the exponents, base 2), sum
   float* part_o;           // [part][row][D], relative to the part's maximum
   int32_t num_pages, hkv, hq, batch, total_q, part_rows;
-  int32_t behind;          // whether cut q tiles of more than 16 rows are left to merge8_kernel
+  int32_t spans;           // workgroups
   float scale_log2;        // softmax scale x log2(e)
 };
 
@@ -269,8 +315,10 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(
 // As assembly so that the compiler does not wait for them before LDS reads of other buffers; they are waited for
 // by count before the barrier that publishes them.  (The s_nop: five wait states between a vector instruction that
 // writes a scalar register, which the address may come from, and a memory instruction that reads it.)
-__device__ __forceinline__ void copy16_to_lds(const char* base, uint32_t lane_off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1"
+// (The first: 2 KiB, a block, the instruction's offset moving both addresses.)
+__device__ __forceinline__ void copy_block_to_lds(const char* base, uint32_t lane_off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1\n\t"
+               "global_load_lds_dwordx4 %0, %1 offset:1024"
                :: "v"(lane_off), "s"(base), "s"(lds_base) : "memory", "m0");
 }
 __device__ __forceinline__ void copy4_to_lds(const void* base, uint32_t lane_off, uint32_t lds_base) {
@@ -286,13 +334,14 @@ struct Piece {
   int kv_len;                        // keys the tile's last token sees
 };
 
-constexpr int kStages = 3;
+constexpr int kStages = 4;
 constexpr int kTileBytes = 4 * 2 * kBlockBytes;         // codes of a KV tile: page by page, K then V
 constexpr int kScaleBytes = 4 * 256;                    // its scales: page by page, K and V in turns (256 bytes land)
 constexpr int kStageBytes = kTileBytes + kScaleBytes;
 constexpr int kOStride = kHeadDim + 4;                  // floats between rows of O in LDS (few rows)
 constexpr int kFewBytes = 4 * kFewRows * kOStride * 4 + 4 * kFewRows * 8;
-constexpr int kLdsBytes = kStages * kStageBytes > kFewBytes ? kStages * kStageBytes : kFewBytes;
+constexpr int kLdsBytes = kStages * kStageBytes;
+static_assert(kLdsBytes >= kFewBytes && (kStages & (kStages - 1)) == 0, "areas that share the LDS; a ring by masks");
 
 // Address of a page's codes of one kv head's K; V lies hkv blocks behind
 __device__ __forceinline__ int64_t page_offset(const Attn8Args& a, int page, int hk) {
@@ -318,8 +367,8 @@ struct Parts {
   buffer_rsrc o, ml;
   int rows;
   __device__ __forceinline__ explicit Parts(const Attn8Args& a)
-      : o(make_rsrc(a.part_o, 2ll * kSpans * a.part_rows * kHeadDim * 4)),
-        ml(make_rsrc(a.part_ml, 2ll * kSpans * a.part_rows * 8)), rows(a.part_rows) {}
+      : o(make_rsrc(a.part_o, 2ll * a.spans * a.part_rows * kHeadDim * 4)),
+        ml(make_rsrc(a.part_ml, 2ll * a.spans * a.part_rows * 8)), rows(a.part_rows) {}
   __device__ __forceinline__ uint32_t at(int part, int row) const { return (uint32_t)(part * rows + row); }
   template <int kScope>
   __device__ __forceinline__ void put(uint32_t i, int d, f32x4 v) const {
@@ -419,7 +468,8 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
     }
     float mx = s[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
+    for (int i = 1; i < 15; i += 2) mx = max3(mx, s[i >> 2][i & 3], s[(i + 1) >> 2][(i + 1) & 3]);
+    mx = max3(mx, mx, s[3][3]);
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32)) * c2;
     if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
@@ -455,34 +505,15 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
           some |= nan_codes(vc[i][j]);
         }
       if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {
-        // 0 x NaN: such codes count for the rows that see their key, and for no other.  They are counted by a
-        // product of their places and the keys seen, and taken out of V.
-        vec8 seen[2];
+        bf16x8 seen[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          u32x4 w;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = key0 + 8 * h + 2 * j;
-            w[j] = (key <= my_pos ? Num<T>::kOne : 0u) | (key + 1 <= my_pos ? Num<T>::kOne << 16 : 0u);
-          }
-          seen[h] = __builtin_bit_cast(vec8, w);
-        }
+        for (int e = 0; e < 2; ++e) seen[e] = keys_seen(key0 + 8 * e, my_pos);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          u32x4 at;
+          const u32x4 at = take_nan_codes(vc[i]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t b = nan_codes(vc[i][j]) >> 7;
-            at[j] = b * 0x38u;           // the code of 1
-            vc[i][j] &= ~(b * 0xffu);
-          }
-          f32x4 n = {0.f, 0.f, 0.f, 0.f};
-          n = Num<T>::mfma16(numbers<T>(at[0], at[1], 1.f), seen[0], n);
-          n = Num<T>::mfma16(numbers<T>(at[2], at[3], 1.f), seen[1], n);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (n[r] > 0.f) o[i][r] = __builtin_nanf("");
+          for (int e = 0; e < 4; ++e)
+            o[i] = Num<__bf16>::mfma16(huge(at, e & 1, e < 2), seen[e & 1], o[i]);
         }
       }
     }
@@ -539,48 +570,48 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
 }
 
 // ---- 128 rows ---------------------------------------------------------------------------------
-// Each wavefront has 32 rows and walks all keys of the piece, on v_mfma_f32_32x32x16.  KV tiles are copied
-// as they lie into a ring of LDS buffers, and every wavefront converts what it reads.  Lane l, n = l % 32,
-// h = l / 32: matrix row i of S^T is slot (i / 8) * 4 + i % 4 of page (i / 4) % 2 of a pair, so a lane ends up with
-// the 16 scores of page h and query row n, and V^T is 16 contiguous bytes of that page.
+// Bound by the matrix and the vector pipes.  Each wavefront has 32 rows and walks all keys of the piece, a half tile (32 keys,
+// two pages) at a time, on v_mfma_f32_32x32x16; two workgroups share a compute unit.  KV tiles are copied as
+// they lie into a ring of LDS buffers, and every wavefront converts what it reads.  Lane l, n = l % 32, h = l / 32:
+// matrix row i of S^T is slot (i / 8) * 4 + i % 4 of page (i / 4) % 2 of the half tile, so a lane ends up with the 16 scores
+// of page h and query row n, P^T is the second product's operand as it lies, and V^T is 16 contiguous bytes of page h.
 // K rows are 128 bytes, 8 chunks of 16; chunk c of slot s of page g lies at c ^ (s % 4 + 4 (g % 2)): any 8
 // neighbouring lanes of a K read then hit 8 different chunks, so all banks.  V reads are contiguous.
+//   half step  phase 1: S of the next half on the matrix pipe; beside it half of this one's exponentials and K's conversion
+//              phase 2: O^T += V^T P^T; beside it the other half, the row maxima of the next S, V's conversion
+// The order within a phase is pinned: a matrix instruction, then what fits beside it.
 template <typename T, int G>
 __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, const Target& to, char* lds) {
   typedef typename Num<T>::vec8 vec8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const int row = wave * 32 + n, tok = min(row / G, p.ntok - 1);
+  const int row = wave * 32 + n, tok = min(row / G, p.ntok - 1), my_pos = p.first_pos + tok;
   const bool active = wave * 32 < p.ntok * G;
-  const int my_pos = p.first_pos + tok;
   const float c2 = a.scale_log2;
   const uint32_t lds0 = lds_addr(lds);
 
   // this wavefront copies page `wave` of every tile
   const int32_t* table = a.page_table + p.table_off;
   int ids = 0, ids_t = p.t0 - 64;        // lane i holds the page id of tile ids_t + i
-  const uint32_t lane16 = lane * 16;
-  uint32_t k_off[2];                     // where in a K block a lane's 16 bytes come from
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int slot = 8 * i + (lane >> 3);
-    k_off[i] = slot * kHeadDim + (((lane & 7) ^ ((slot & 3) | (wave & 1) << 2)) << 4);
-  }
+  // where in the page a lane's 16 bytes of the K (V) block's halves come from
+  const uint32_t k_from = (lane >> 3) * kHeadDim + (((lane & 7) ^ ((lane >> 3 & 3) | (wave & 1) << 2)) << 4);
+  const uint32_t v_from = a.hkv * kBlockBytes + lane * 16;
+  const char* codes = a.codes + (int64_t)p.hk * kBlockBytes;
+  const float* scales = a.scales + 2 * p.hk;
+  const uint32_t page_stride = 2u * a.hkv * kBlockBytes;
+  const uint32_t lds_wave = lds0 + wave * 2 * kBlockBytes, lds_scales = lds0 + kTileBytes + wave * 256;
+  auto stage_at = [&](int t) __attribute__((always_inline)) { return (uint32_t)((t - p.t0) & (kStages - 1)) * kStageBytes; };
   auto copy_tile = [&](int t) __attribute__((always_inline)) {
     if (t >= ids_t + 64) {
       ids_t = t;
       ids = table[min(4 * (t + lane) + wave, p.last_entry)];
     }
     const int page = min(max(__builtin_amdgcn_readlane(ids, t - ids_t), 0), a.num_pages - 1);
-    const char* k = a.codes + ((int64_t)page * 2 * a.hkv + p.hk) * kBlockBytes;
-    const char* v = k + (int64_t)a.hkv * kBlockBytes;
-    const uint32_t to_lds = lds0 + (t - p.t0) % kStages * kStageBytes + wave * 2 * kBlockBytes;
-    copy16_to_lds(k, k_off[0], to_lds);
-    copy16_to_lds(k, k_off[1], to_lds + 1024);
-    copy16_to_lds(v, lane16, to_lds + kBlockBytes);
-    copy16_to_lds(v, lane16 + 1024, to_lds + kBlockBytes + 1024);
-    copy4_to_lds(a.scales + ((int64_t)page * a.hkv + p.hk) * 2, (lane & 1) * 4,
-                 lds0 + (t - p.t0) % kStages * kStageBytes + kTileBytes + wave * 256);
+    const char* from = codes + (uint64_t)(uint32_t)page * page_stride;
+    const uint32_t stage = stage_at(t);
+    copy_block_to_lds(from, k_from, lds_wave + stage);
+    copy_block_to_lds(from, v_from, lds_wave + stage + kBlockBytes);
+    copy4_to_lds(scales + (uint64_t)(uint32_t)page * (2u * a.hkv), (lane & 1) * 4, lds_scales + stage);
   };
   constexpr int kCopies = 5;             // of a wavefront and tile
 
@@ -592,55 +623,82 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     for (int u = 0; u < 8; ++u)
       q[u] = *reinterpret_cast<const vec8*>(from + ((u >> 1) * 32 + h * 16 + (u & 1) * 8) * 2);
   }
-  f32x16 o[4];
+  f32x16 o[4], s_a, s_b;
   const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = zero;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, mx = -INFINITY;
+
+  // LDS offsets of this lane's fragments within a stage, of half tile 0; half tile 1 lies two pages behind
+  const int k_page = n >> 2 & 1, k_slot = (n >> 3) * 4 + (n & 3);
+  const uint32_t k_off = k_page * 2 * kBlockBytes + k_slot * kHeadDim + ((h ^ ((k_slot & 3) | k_page << 2)) << 4);
+  const uint32_t v_off = h * 2 * kBlockBytes + kBlockBytes + n * kPage;
+  const uint32_t ks_off = kTileBytes + k_page * 256, vs_off = kTileBytes + h * 256 + 4;
+  u32x4 kc[4], vc[4];                    // raw codes: of the next half's K, of this half's V
+  float ks;
+  auto load_k = [&](uint32_t stage, int half, int cc) __attribute__((always_inline)) {
+    kc[cc] = *reinterpret_cast<const u32x4*>(lds + stage + (k_off ^ (cc << 5)) + half * 4 * kBlockBytes);
+  };
+  auto load_v = [&](uint32_t stage, int half, int i) __attribute__((always_inline)) {
+    vc[i] = *reinterpret_cast<const u32x4*>(lds + stage + v_off + half * 4 * kBlockBytes + i * 32 * kPage);
+  };
+  auto load_ks = [&](uint32_t stage, int half) __attribute__((always_inline)) {
+    ks = *reinterpret_cast<const float*>(lds + stage + ks_off + half * 512);
+  };
+  // lane: scores of keys key0 + 16 h + r
+  auto mask = [&](int key0, f32x16& s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (key0 + 16 * h + r > my_pos) s[r] = -INFINITY;
+  };
+  auto across = [&](float x) __attribute__((always_inline)) {
+    uint32_t lo = __builtin_bit_cast(uint32_t, x), hi = lo;
+    swap_halves(lo, hi);
+    return fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi)) * c2;
+  };
+  // codes of keys behind the last one go; NaN codes count for the rows that see their key (take_nan_codes)
+  auto mend_v = [&](int key0) __attribute__((always_inline)) {
+    const int first = key0 + 16 * h, valid = min(max(p.kv_len - first, 0), 16);
+    uint32_t some = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int kept = min(max(valid - 4 * j, 0), 4);
+        vc[i][j] &= kept == 4 ? 0xffffffffu : (1u << (8 * kept)) - 1u;
+        some |= nan_codes(vc[i][j]);
+      }
+    if (__builtin_amdgcn_ballot_w64(some != 0) == 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 at = take_nan_codes(vc[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o[i] = Num<__bf16>::mfma32(huge(at, e & 1, e < 2), keys_seen(first + 8 * (e & 1), my_pos), o[i]);
+    }
+  };
 
   __syncthreads();                       // (earlier readers of the LDS are done)
-  if (p.t0 < p.t1) copy_tile(p.t0);
-  if (p.t0 + 1 < p.t1) copy_tile(p.t0 + 1);
-  for (int t = p.t0; t < p.t1; ++t) {
-    // (a look-up of page ids in between makes the compiler wait for more: never for less)
-    if (t + 1 < p.t1)
+  for (int i = 0; i < kStages - 1; ++i)
+    if (p.t0 + i < p.t1) copy_tile(p.t0 + i);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  // Tile t + 1 is there, for every wavefront, and none reads tile t - 1 any more.
+  auto turn = [&](int t) __attribute__((always_inline)) {
+    if (t + 2 < p.t1)
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies) : "memory");
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (t + 2 < p.t1) copy_tile(t + 2);
-    if (!active) continue;
-    const char* stage = lds + (t - p.t0) % kStages * kStageBytes;
-    const float* sc = reinterpret_cast<const float*>(stage + kTileBytes);
-    const int key0 = t * kBN;
-    const bool masked = key0 + kBN - 1 > p.first_pos;
-    f32x16 s[2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      // A row n: slot (n / 8) * 4 + n % 4 of page 2 b + (n / 4) % 2
-      const int pg = 2 * b + ((n >> 2) & 1), slot = (n >> 3) * 4 + (n & 3);
-      const float ks = sc[pg * 64];
-      const char* from = stage + pg * 2 * kBlockBytes + slot * kHeadDim;
-      s[b] = zero;
-#pragma unroll
-      for (int cc = 0; cc < 4; ++cc) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(from + (((2 * cc + h) ^ ((slot & 3) | (pg & 1) << 2)) << 4));
-        s[b] = Num<T>::mfma32(numbers<T>(w[0], w[1], ks), q[2 * cc], s[b]);
-        s[b] = Num<T>::mfma32(numbers<T>(w[2], w[3], ks), q[2 * cc + 1], s[b]);
-      }
-    }
-    // lane: scores of keys key0 + 32 b + 16 h + r
-    if (masked) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key0 + 32 * b + 16 * h + r > my_pos) s[b][r] = -INFINITY;
-    }
-    float mx = s[0][0];
-#pragma unroll
-    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32)) * c2;
+    if (t + kStages - 1 < p.t1) copy_tile(t + kStages - 1);
+  };
+
+  // s: scores of keys key0 .. key0 + 31, s_next: of the 32 behind them, whose codes are in kc
+  auto half_step = [&](int t, auto which, f32x16& s, f32x16& s_next) __attribute__((always_inline)) {
+    constexpr int kHalf = decltype(which)::value;
+    const int key0 = t * kBN + 32 * kHalf;
+    const uint32_t stage = stage_at(t), next = stage_at(t + 1);   // (behind the last tile: stale, and not used)
+    // the rows' reference moves when a maximum has risen by more than 2^8
     if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
       const float m_new = fmaxf(m, mx);
       const float f = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -650,66 +708,93 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       for (int i = 0; i < 4; ++i) o[i] *= f;
     }
     const float ref = m == -INFINITY ? 0.f : m;
-    vec8 pt[2][2];
+    uint32_t pk[8];
+    float e0, e1;
+    auto soft_exp = [&](int i) __attribute__((always_inline)) {
+      e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i], c2, -ref));
+      e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * i + 1], c2, -ref));
+    };
+    auto soft_sum = [&](int i) __attribute__((always_inline)) {
+      l += e0 + e1;
+      pk[i] = pack2<T>(e0, e1);
+      asm volatile("" : "+v"(l), "+v"(pk[i]));     // (stays in this phase)
+    };
+    vec8 op = numbers<T>(kc[0][0], kc[0][1], ks);
+    __builtin_amdgcn_sched_barrier(0);
+    // ---- phase 1: words 0..3 of P are made on the way
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        u32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * e + 2 * j], c2, -ref));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * e + 2 * j + 1], c2, -ref));
-          l += p0 + p1;
-          w[j] = pack2<T>(p0, p1);
-        }
-        pt[b][e] = __builtin_bit_cast(vec8, w);
+    for (int u = 0; u < 8; ++u) {
+      s_next = Num<T>::mfma32(op, q[u], u == 0 ? zero : s_next);
+      if (u & 1) soft_sum(u >> 1);
+      else soft_exp(u >> 1);
+      if (u < 7) {
+        const u32x4& w = kc[(u + 1) >> 1];
+        op = numbers<T>(w[2 * ((u + 1) & 1)], w[2 * ((u + 1) & 1) + 1], ks);
       }
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int pg = 2 * b + h;
-      const float vs = sc[pg * 64 + 1];
-      const char* from = stage + pg * 2 * kBlockBytes + kBlockBytes + n * kPage;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u32x4 w = *reinterpret_cast<const u32x4*>(from + i * 32 * kPage);
-        if (masked) {
-          const int first = key0 + 32 * b + 16 * h, valid = min(max(p.kv_len - first, 0), 16);
-          uint32_t some = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int kept = min(max(valid - 4 * j, 0), 4);
-            w[j] &= kept == 4 ? 0xffffffffu : (1u << (8 * kept)) - 1u;
-            some |= nan_codes(w[j]);
-          }
-          if (__builtin_amdgcn_ballot_w64(some != 0) != 0) {      // (as in few_rows_piece)
-            f32x16 cnt = zero;
-            u32x4 at;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t x = nan_codes(w[j]) >> 7;
-              at[j] = x * 0x38u;
-              w[j] &= ~(x * 0xffu);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              u32x4 seen;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int key = first + 8 * e + 2 * j;
-                seen[j] = (key <= my_pos ? Num<T>::kOne : 0u) | (key + 1 <= my_pos ? Num<T>::kOne << 16 : 0u);
-              }
-              cnt = Num<T>::mfma32(numbers<T>(at[2 * e], at[2 * e + 1], 1.f), __builtin_bit_cast(vec8, seen), cnt);
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (cnt[r] > 0.f) o[i][r] = __builtin_nanf("");
-          }
-        }
-        o[i] = Num<T>::mfma32(numbers<T>(w[0], w[1], vs), pt[b][0], o[i]);
-        o[i] = Num<T>::mfma32(numbers<T>(w[2], w[3], vs), pt[b][1], o[i]);
-      }
+      if (u >= 2 && u < 6) load_v(stage, kHalf, u - 2);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    const float vs = *reinterpret_cast<const float*>(lds + stage + vs_off + kHalf * 512);
+    if constexpr (kHalf == 0) turn(t);
+    // (the empty statements keep the compiler from doing either always, by selects)
+    if (key0 + 63 > p.first_pos) {
+      asm volatile("");
+      mask(key0 + 32, s_next);
+    }
+    if (key0 + 31 > p.first_pos) {
+      asm volatile("");
+      mend_v(key0);
+    }
+    // ---- phase 2: V's d blocks with keys 0..7 of the page, then with keys 8..15
+    op = numbers<T>(vc[0][0], vc[0][1], vs);
+    float x = -INFINITY;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int e = u >> 2;
+      const u32x4 pw = {pk[4 * e], pk[4 * e + 1], pk[4 * e + 2], pk[4 * e + 3]};
+      o[u & 3] = Num<T>::mfma32(op, __builtin_bit_cast(vec8, pw), o[u & 3]);
+      if (u < 4) {
+        soft_exp(4 + u);
+        soft_sum(4 + u);
+        // the half behind the next: of this tile's successor
+        if constexpr (kHalf == 0) load_k(next, 0, u);
+        else load_k(next, 1, u);
+      } else {
+        x = max3(x, s_next[4 * (u - 4)], s_next[4 * (u - 4) + 1]);
+        x = max3(x, s_next[4 * (u - 4) + 2], s_next[4 * (u - 4) + 3]);
+      }
+      if (u < 7) {
+        const u32x4& w = vc[(u + 1) & 3];
+        op = numbers<T>(w[2 * ((u + 1) >> 2)], w[2 * ((u + 1) >> 2) + 1], vs);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    load_ks(next, kHalf);
+    mx = across(x);
+  };
+  if (active && p.t0 < p.t1) {
+    const uint32_t stage = stage_at(p.t0);
+    load_ks(stage, 0);
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) load_k(stage, 0, cc);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      s_a = Num<T>::mfma32(numbers<T>(kc[u >> 1][2 * (u & 1)], kc[u >> 1][2 * (u & 1) + 1], ks), q[u], u == 0 ? zero : s_a);
+    if (p.t0 * kBN + 31 > p.first_pos) mask(p.t0 * kBN, s_a);
+    float x = s_a[0];
+#pragma unroll
+    for (int i = 1; i < 15; i += 2) x = max3(x, s_a[i], s_a[i + 1]);
+    mx = across(max3(x, x, s_a[15]));
+    load_ks(stage, 1);
+#pragma unroll
+    for (int cc = 0; cc < 4; ++cc) load_k(stage, 1, cc);
+    for (int t = p.t0; t < p.t1; ++t) {
+      half_step(t, std::integral_constant<int, 0>(), s_a, s_b);
+      half_step(t, std::integral_constant<int, 1>(), s_b, s_a);
+    }
+  } else {
+    for (int t = p.t0; t < p.t1; ++t) turn(t);
   }
   l += __shfl_xor(l, 32);
   if (row >= p.ntok * G) return;
@@ -717,30 +802,27 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   if (to.part >= 0) {
     const Parts parts(a);
     const uint32_t at = parts.at(to.part, row);
-    auto store = [&](auto scope) __attribute__((always_inline)) {
-      constexpr int kScope = decltype(scope)::value;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          parts.put<kScope>(at, 32 * i + 8 * j + 4 * h,
-                            f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
-      if (h == 0) parts.put_ml<kScope>(at, m, l);
-    };
-    if (a.behind)
-      store(std::integral_constant<int, kLaunchScope>());
-    else
-      store(std::integral_constant<int, kDeviceScope>());
+      for (int j = 0; j < 4; ++j)
+        parts.put<kLaunchScope>(at, 32 * i + 8 * j + 4 * h,
+                                f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
+    if (h == 0) parts.put_ml<kLaunchScope>(at, m, l);
   } else {
     const int64_t at = out_row<G>(a, p, row);
     const float inv = 1.f / l;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<u32x2*>(a.out + at * kRowBytes + (32 * i + 8 * j + 4 * h) * 2) =
-            u32x2{pack2<T>(o[i][4 * j] * inv, o[i][4 * j + 1] * inv),
-                  pack2<T>(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv)};
+      for (int j = 0; j < 4; j += 2) {
+        // the lane with h = 0 gets the row's 16 bytes of j, the other those of j + 1
+        uint32_t x0 = pack2<T>(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), x1 = pack2<T>(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv);
+        uint32_t y0 = pack2<T>(o[i][4 * j + 4] * inv, o[i][4 * j + 5] * inv), y1 = pack2<T>(o[i][4 * j + 6] * inv, o[i][4 * j + 7] * inv);
+        swap_halves(x0, y0);
+        swap_halves(x1, y1);
+        *reinterpret_cast<u32x4*>(a.out + at * kRowBytes + (32 * i + 8 * (j + h)) * 2) = u32x4{x0, x1, y0, y1};
+      }
     if (h == 0) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
 }
@@ -804,7 +886,7 @@ __global__ __launch_bounds__(kThreads) void merge8_kernel(Attn8Args a) {
     return;
   const int w = blockIdx.x / kMergeBlocks;
   const MergeRec8 r = a.merges[w];
-  if (r.count < 2 || w + r.count > kSpans) return;
+  if (r.count < 2 || w + r.count > a.spans) return;
   Piece p = {};
   p.hk = r.hk;
   p.q_first = r.q_first;
@@ -812,18 +894,20 @@ __global__ __launch_bounds__(kThreads) void merge8_kernel(Attn8Args a) {
   combine<T, G, kLaunchScope, 4>(a, p, w, r.count, blockIdx.x % kMergeBlocks * 16, 16 * kMergeBlocks);
 }
 
-template <typename T, int G>
+template <typename T, int G, bool kFewOnly>
 __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
-  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
+  __shared__ __attribute__((aligned(1024))) char lds[kFewOnly ? kFewBytes : kLdsBytes];
   __shared__ int s_last;
+  constexpr int kRows = kFewOnly ? kFewRows : kTileRows;
   const Plan8Header hdr = *a.hdr;
   // the plan must be one of this very batch
-  if (hdr.magic != kPlanMagic || hdr.heads != a.hkv * 16 + G || hdr.batch != a.batch || hdr.total_q != a.total_q)
+  if (hdr.magic != kPlanMagic || hdr.heads != a.hkv * 16 + G || hdr.batch != a.batch || hdr.total_q != a.total_q ||
+      hdr.tile_rows != kRows)
     return;
   const int64_t visits = hdr.visits, span = hdr.span;
   // neighbouring spans, which share K and V, on one XCD (workgroups go to the XCDs in turns)
-  const int w = blockIdx.x % kXcds * (kSpans / kXcds) + blockIdx.x / kXcds;
-  if (a.behind && threadIdx.x == 0) a.merges[w].count = 0;
+  const int w = blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds;
+  if (!kFewOnly && threadIdx.x == 0) a.merges[w].count = 0;
   int64_t at = w * span;
   const int64_t end = min(at + span, visits * a.hkv);
   if (at >= end) return;
@@ -846,7 +930,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   int64_t tile = 0;
   {
     const int64_t left = in_head - a.cum[s];
-    const int q = a.seqs[s].q, tok = tile_tokens<G>(q);
+    const int q = a.seqs[s].q, tok = rows_of_tiles(q, G, kRows) / G;
     int64_t cnt = (q + tok - 1) / tok;
     while (cnt > 1) {
       const int64_t half = cnt / 2;
@@ -860,7 +944,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   }
   while (at < end) {
     const PlanSeq sq = a.seqs[s];
-    const int q0 = sq.q_first, q = sq.q, tok = tile_tokens<G>(q), b = sq.begin;
+    const int q0 = sq.q_first, q = sq.q, tok = rows_of_tiles(q, G, kRows) / G, b = sq.begin;
+    const bool few = kFewOnly || tok == kFewRows / G;
     const int row0 = (int)tile * tok, ntok = min(tok, q - row0);
     const int planned = (int)tiles64((int64_t)b + row0 + ntok);     // KV tiles of this q tile, by the plan
     const int64_t tile_at = hk * visits + a.cum[s] + visits_before(b, q, tok, tile);
@@ -884,13 +969,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     if (ok) {
       Target to;
       to.part = whole ? -1 : 2 * w + (t0 == 0 ? 1 : 0);
-      if (few_rows(q, G))
+      if (few)
         few_rows_piece<T, G>(a, p, to, lds);
-      else
+      else if constexpr (!kFewOnly)
         tile_piece<T, G>(a, p, to, lds);
       if (!whole) {
         const int w0 = (int)(tile_at / span), count = (int)((tile_at + planned - 1) / span) - w0 + 1;
-        if (a.behind && !few_rows(q, G)) {
+        if (!few) {
           if (t0 == 0 && threadIdx.x == 0) a.merges[w] = MergeRec8{p.q_first, p.ntok, p.hk, count};
         } else {
           asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wavefront's rows have been written
@@ -938,19 +1023,23 @@ mc_status check_shape8(const mc_pool8_desc* pool, int32_t num_q_heads, int32_t b
 }
 
 template <typename T>
-mc_status launch_attn8(int G, hipStream_t hs, const Attn8Args& a) {
-  auto* kernel = G == 1   ? attn8_kernel<T, 1>
-                 : G == 2 ? attn8_kernel<T, 2>
-                 : G == 4 ? attn8_kernel<T, 4>
-                          : attn8_kernel<T, 8>;
-  hipLaunchKernelGGL(kernel, dim3(kSpans), dim3(kThreads), 0, hs, a);
-  mc_status st = mc::launch_status();
-  if (st != MC_OK || !a.behind) return st;
+mc_status launch_attn8(int G, bool few, hipStream_t hs, const Attn8Args& a) {
+  auto* kernel = few ? (G == 1   ? attn8_kernel<T, 1, true>
+                        : G == 2 ? attn8_kernel<T, 2, true>
+                        : G == 4 ? attn8_kernel<T, 4, true>
+                                 : attn8_kernel<T, 8, true>)
+                     : (G == 1   ? attn8_kernel<T, 1, false>
+                        : G == 2 ? attn8_kernel<T, 2, false>
+                        : G == 4 ? attn8_kernel<T, 4, false>
+                                 : attn8_kernel<T, 8, false>);
+  hipLaunchKernelGGL(kernel, dim3(a.spans), dim3(kThreads), 0, hs, a);
+  const mc_status st = mc::launch_status();
+  if (st != MC_OK || few) return st;
   auto* merge = G == 1   ? merge8_kernel<T, 1>
                 : G == 2 ? merge8_kernel<T, 2>
                 : G == 4 ? merge8_kernel<T, 4>
                          : merge8_kernel<T, 8>;
-  hipLaunchKernelGGL(merge, dim3(kSpans * kMergeBlocks), dim3(kThreads), 0, hs, a);
+  hipLaunchKernelGGL(merge, dim3(a.spans * kMergeBlocks), dim3(kThreads), 0, hs, a);
   return mc::launch_status();
 }
 
@@ -994,6 +1083,8 @@ mc_status mc_attn8_plan_ahead(const mc_pool8_desc* pool, int32_t num_q_heads, in
   a.hkv = pool->num_kv_heads;
   a.G = G;
   a.ahead = ahead_tokens;
+  a.tile_rows = w.few ? kFewRows : kTileRows;
+  a.spans = w.spans;
   hipLaunchKernelGGL(plan8_kernel, dim3(1 + (unsigned)batch), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
   return mc::launch_status();
 }
@@ -1067,12 +1158,11 @@ mc_status mc_prefix_prefill_attn8(const mc_pool8_desc* pool, int32_t layer, cons
   a.batch = batch;
   a.total_q = total_q;
   a.part_rows = w.part_rows;
-  // (more than one new token for a sequence on average: some may be q tiles of many rows)
-  a.behind = total_q > batch && (int64_t)total_q * G > kFewRows;
+  a.spans = w.spans;
   const float scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)kHeadDim);
   a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  return pool->dtype == MC_F16 ? launch_attn8<_Float16>(G, hs, a) : launch_attn8<__bf16>(G, hs, a);
+  return pool->dtype == MC_F16 ? launch_attn8<_Float16>(G, w.few, hs, a) : launch_attn8<__bf16>(G, w.few, hs, a);
 }
 
 }  // extern "C"
