@@ -29,6 +29,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;     // 4 wavefronts
 constexpr int kTileRows = 128, kFewRows = 16;
@@ -569,6 +570,59 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
   }
 }
 
+// ---- Q in codes -------------------------------------------------------------------------------
+// K Q^T can take K's codes as they are: the matrix instructions for scaled 8-bit numbers multiply a row by
+// a power of two of its own, which is what K's scales are.  A bf16 number has 8 significant bits and a code 4, so Q becomes
+// two rows of codes, hi and lo = the rest, lo at a 16th of hi's scale, with a scale per 64 numbers.  hi + lo is the number exactly
+// unless it is below 2^-14 of the largest of its 64; then it is off by at most 2^-23 of that, the size of
+// an fp32 rounding of it.  Two products of twice the rate take the matrix pipe's time of one in bf16, and K's
+// conversion, a fifth of the vector instructions of a half step, goes.  (fp16 numbers have 11 bits: three rows
+// would cost more than the conversion.)
+struct CodedQ {
+  i32x8 hi[2], lo[2];    // of d block j: 32 numbers of a lane, the other 32 in the row's other lane
+  int scales;            // exponents (E8M0): hi and lo of block 0, of block 1
+};
+__device__ __forceinline__ f32x16 mfma_coded(u32x4 k0, u32x4 k1, int k_scale, i32x8 q, int q_scales, int which, f32x16 c) {
+  const i32x8 k = {(int)k0[0], (int)k0[1], (int)k0[2], (int)k0[3], (int)k1[0], (int)k1[1], (int)k1[2], (int)k1[3]};
+  switch (which) {       // (the byte of q_scales is part of the instruction)
+    case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 0, q_scales);
+    case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 1, q_scales);
+    case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 2, q_scales);
+    default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 3, q_scales);
+  }
+}
+// q: bf16 numbers, vector 4 j + i the numbers 8 i + [0, 8) of block j
+__device__ __forceinline__ CodedQ code_q(const bf16x8 (&q)[8]) {
+  CodedQ r;
+  r.scales = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) big = max(big, mc::magnitude((float)q[4 * j + (i >> 3)][i & 7]));
+    uint32_t other = big;
+    swap_halves(big, other);             // (both lanes of a row: one scale for the block's 64 numbers)
+    const int k = mc::scale_exponent(max(big, other), mc::ScaleLimits{-100, 120});
+    const float inv = mc::power_of_two(-k);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      float x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (float)q[4 * j + (w >> 1)][4 * (w & 1) + i] * inv;
+      const uint32_t hi = mc::four_codes(x[0], x[1], x[2], x[3]);
+      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
+      y[0] = (x[0] - a[0]) * 16.f;
+      y[1] = (x[1] - a[1]) * 16.f;
+      y[2] = (x[2] - b[0]) * 16.f;
+      y[3] = (x[3] - b[1]) * 16.f;
+      r.hi[j][w] = (int)hi;
+      r.lo[j][w] = (int)mc::four_codes(y[0], y[1], y[2], y[3]);
+    }
+    r.scales |= ((k + 127) | (k + 127 - 4) << 8) << (16 * j);
+  }
+  return r;
+}
+
 // ---- 128 rows ---------------------------------------------------------------------------------
 // Bound by the matrix and the vector pipes.  Each wavefront has 32 rows and walks all keys of the piece, a half tile (32 keys,
 // two pages) at a time, on v_mfma_f32_32x32x16; two workgroups share a compute unit.  KV tiles are copied as
@@ -577,7 +631,8 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
 // of page h and query row n, P^T is the second product's operand as it lies, and V^T is 16 contiguous bytes of page h.
 // K rows are 128 bytes, 8 chunks of 16; chunk c of slot s of page g lies at c ^ (s % 4 + 4 (g % 2)): any 8
 // neighbouring lanes of a K read then hit 8 different chunks, so all banks.  V reads are contiguous.
-//   half step  phase 1: S of the next half on the matrix pipe; beside it half of this one's exponentials and K's conversion
+//   half step  phase 1: S of the next half on the matrix pipe; beside it this one's exponentials (in fp16: half of them, and
+//                       K's conversion)
 //              phase 2: O^T += V^T P^T; beside it the other half, the row maxima of the next S, V's conversion
 // The order within a phase is pinned: a matrix instruction, then what fits beside it.
 template <typename T, int G>
@@ -623,6 +678,9 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     for (int u = 0; u < 8; ++u)
       q[u] = *reinterpret_cast<const vec8*>(from + ((u >> 1) * 32 + h * 16 + (u & 1) * 8) * 2);
   }
+  constexpr bool kCoded = std::is_same<T, __bf16>::value;
+  CodedQ cq;
+  if constexpr (kCoded) cq = code_q(q);
   f32x16 o[4], s_a, s_b;
   const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
@@ -719,9 +777,27 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       pk[i] = pack2<T>(e0, e1);
       asm volatile("" : "+v"(l), "+v"(pk[i]));     // (stays in this phase)
     };
-    vec8 op = numbers<T>(kc[0][0], kc[0][1], ks);
+    vec8 op;
+    // ---- phase 1: words 0..3 (all) of P are made on the way
+    constexpr int kEarly = kCoded ? 8 : 4;
+    if constexpr (kCoded) {
+      const int k_scale = __builtin_bit_cast(uint32_t, ks) >> 23;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = u >> 1;
+        s_next = mfma_coded(kc[2 * j], kc[2 * j + 1], k_scale, u & 1 ? cq.lo[j] : cq.hi[j], cq.scales, u, u == 0 ? zero : s_next);
+        asm volatile("" ::"v"(s_next));            // (stays in this phase)
+        soft_exp(2 * u);
+        soft_sum(2 * u);
+        soft_exp(2 * u + 1);
+        soft_sum(2 * u + 1);
+        load_v(stage, kHalf, u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+    op = numbers<T>(kc[0][0], kc[0][1], ks);
     __builtin_amdgcn_sched_barrier(0);
-    // ---- phase 1: words 0..3 of P are made on the way
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       s_next = Num<T>::mfma32(op, q[u], u == 0 ? zero : s_next);
@@ -733,6 +809,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       }
       if (u >= 2 && u < 6) load_v(stage, kHalf, u - 2);
       __builtin_amdgcn_sched_barrier(0);
+    }
     }
     const float vs = *reinterpret_cast<const float*>(lds + stage + vs_off + kHalf * 512);
     if constexpr (kHalf == 0) turn(t);
@@ -755,8 +832,10 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       const u32x4 pw = {pk[4 * e], pk[4 * e + 1], pk[4 * e + 2], pk[4 * e + 3]};
       o[u & 3] = Num<T>::mfma32(op, __builtin_bit_cast(vec8, pw), o[u & 3]);
       if (u < 4) {
-        soft_exp(4 + u);
-        soft_sum(4 + u);
+        if constexpr (kEarly < 8) {
+          soft_exp(4 + u);
+          soft_sum(4 + u);
+        }
         // the half behind the next: of this tile's successor
         if constexpr (kHalf == 0) load_k(next, 0, u);
         else load_k(next, 1, u);
@@ -778,6 +857,12 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     load_ks(stage, 0);
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) load_k(stage, 0, cc);
+    if constexpr (kCoded) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        s_a = mfma_coded(kc[u & 2], kc[(u & 2) + 1], __builtin_bit_cast(uint32_t, ks) >> 23,
+                         u & 1 ? cq.lo[u >> 1] : cq.hi[u >> 1], cq.scales, u, u == 0 ? zero : s_a);
+    } else
 #pragma unroll
     for (int u = 0; u < 8; ++u)
       s_a = Num<T>::mfma32(numbers<T>(kc[u >> 1][2 * (u & 1)], kc[u >> 1][2 * (u & 1) + 1], ks), q[u], u == 0 ? zero : s_a);
