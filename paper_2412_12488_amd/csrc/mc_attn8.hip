@@ -766,6 +766,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       for (int i = 0; i < 4; ++i) o[i] *= f;
     }
     const float ref = m == -INFINITY ? 0.f : m;
+    const float vs = *reinterpret_cast<const float*>(lds + stage + vs_off + kHalf * 512);
     uint32_t pk[8];
     float e0, e1;
     auto soft_exp = [&](int i) __attribute__((always_inline)) {
@@ -811,7 +812,6 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       __builtin_amdgcn_sched_barrier(0);
     }
     }
-    const float vs = *reinterpret_cast<const float*>(lds + stage + vs_off + kHalf * 512);
     if constexpr (kHalf == 0) turn(t);
     // (the empty statements keep the compiler from doing either always, by selects)
     if (key0 + 63 > p.first_pos) {
@@ -823,6 +823,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       mend_v(key0);
     }
     // ---- phase 2: V's d blocks with keys 0..7 of the page, then with keys 8..15
+    load_ks(next, kHalf);
     op = numbers<T>(vc[0][0], vc[0][1], vs);
     float x = -INFINITY;
     __builtin_amdgcn_sched_barrier(0);
@@ -849,7 +850,6 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    load_ks(next, kHalf);
     mx = across(x);
   };
   if (active && p.t0 < p.t1) {
