@@ -3,9 +3,9 @@
 // Work
 //   * A q tile is 128 rows (TOK = 128 / G tokens x the G query heads of one kv head) of one sequence, or all of its
 //     rows where those are at most 16 (decode steps).  A tile walks the 64-key KV tiles that its rows may see.
-//   * All visits of KV tiles by q tiles, kv head after kv head, form one line; plan8_kernel writes down how many
-//     visits lie before each sequence, and the attention launch cuts the line into as many equal spans as
-//     workgroups run at a time.  A span is any mixture of whole q tiles and parts of some; a part's rows (O, maximum, sum)
+//   * All visits of KV tiles by q tiles, kv head after kv head, form one line, each q tile's behind kTileCost units that
+//     stand for what it takes beside them; plan8_kernel writes down how many units lie before each
+//     sequence, and the attention launch cuts the line into as many equal spans as workgroups run at a time.  A span is any mixture of whole q tiles and parts of some; a part's rows (O, maximum, sum)
 //     go to the workspace, and the last workgroup to finish a part of a q tile combines them, in their order.
 //   * Codes become 16-bit numbers in registers, by the instructions that convert two at a time and multiply by the
 //     block's scale (exactly: it is a power of two), and go into the 16-bit matrix instructions.
@@ -36,7 +36,9 @@ constexpr int kTileRows = 128, kFewRows = 16;
 constexpr int kBN = 64;           // keys per KV tile: 4 pages
 constexpr int kSpans = 512;       // workgroups of an attention launch at most: two for each of 256 compute units
 constexpr int kXcds = 8;
-constexpr int kMinSpan = 4;       // visits a span has at least
+constexpr int kMinSpan = 4;       // units a span has at least ...
+// ... and what a q tile takes beside its visits, in visits: looking it up, its Q, its first copies, its rows at the end.
+constexpr int kTileCost = 4;
 constexpr int32_t kPlanMagic = 0x6d63706d;
 
 struct Plan8Header {
@@ -44,8 +46,8 @@ struct Plan8Header {
   int32_t heads;       // kv heads and group size of the plan, as in mc_attn.hip
   int32_t batch;
   int32_t total_q;
-  int64_t visits;      // of all q tiles of one kv head
-  int64_t span;        // visits per workgroup
+  int64_t units;       // of all q tiles of one kv head
+  int64_t span;        // units per workgroup
   int32_t tile_rows;   // rows of a q tile at most: kTileRows, or kFewRows
   int32_t pad[7];
 };
@@ -100,13 +102,13 @@ __device__ __forceinline__ int rows_of_tiles(int q, int G, int tile_rows) {
 }
 __device__ __forceinline__ int64_t tiles64(int64_t keys) { return (keys + kBN - 1) / kBN; }
 
-// Visits of a sequence's first i q tiles, of `tok` tokens each (a power of two): tile j sees the keys before
+// Units of a sequence's first i q tiles, of `tok` tokens each (a power of two): tile j visits the tiles of the keys before
 // b + min((j + 1) tok, q).
-__device__ __forceinline__ int64_t visits_before(int64_t b, int64_t q, int tok, int64_t i) {
-  int64_t n = i, sum = 0;
+__device__ __forceinline__ int64_t units_before(int64_t b, int64_t q, int tok, int64_t i) {
+  int64_t n = i, sum = i * kTileCost;
   if (i * tok > q) {                 // the last tile is short
     n = i - 1;
-    sum = tiles64(b + q);
+    sum += tiles64(b + q);
   }
   if (tok >= kBN) {
     const int64_t r = tok / kBN;
@@ -142,7 +144,7 @@ __device__ __forceinline__ int checked_tokens(const Plan8Args& a, int s, bool* b
   return *bad ? 0 : q1 - q0;
 }
 
-// Workgroup 0 sums the visits; workgroup 1 + s looks at the page ids of sequence s.
+// Workgroup 0 sums the units; workgroup 1 + s looks at the page ids of sequence s.
 __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x > 0) {
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
       const int q = checked_tokens(a, s, &bad);
       if (q > 0) {
         const int tok = rows_of_tiles(q, a.G, a.tile_rows) / a.G;
-        v = visits_before(a.begin[s], q, tok, (q + tok - 1) / tok);
+        v = units_before(a.begin[s], q, tok, (q + tok - 1) / tok);
       }
       a.seqs[s] = PlanSeq{a.begin[s], a.cu_q[s], q, a.cu_pages[s]};
     }
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
     h.heads = a.hkv * 16 + a.G;
     h.batch = a.batch;
     h.total_q = a.total_q;
-    h.visits = before;
+    h.units = before;
     h.span = max((before * a.hkv + a.spans - 1) / a.spans, (int64_t)kMinSpan);
     h.tile_rows = a.tile_rows;
     *a.hdr = h;
@@ -634,7 +636,9 @@ __device__ __forceinline__ CodedQ code_q(const bf16x8 (&q)[8]) {
 //   half step  phase 1: S of the next half on the matrix pipe; beside it this one's exponentials (in fp16: half of them, and
 //                       K's conversion)
 //              phase 2: O^T += V^T P^T; beside it the other half, the row maxima of the next S, V's conversion
-// The order within a phase is pinned: a matrix instruction, then what fits beside it.
+// The order within a phase is pinned: a matrix instruction, then what fits beside it.  Phase 2 has priority: of the two wavefronts
+// of a SIMD the one that came first is otherwise served first throughout, runs ahead, and the other ends alone (16k over
+// 16k tokens: workgroups of 8.4 and 11.1 million cycles, 6.11 ms; with it 5.69).
 template <typename T, int G>
 __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, const Target& to, char* lds) {
   typedef typename Num<T>::vec8 vec8;
@@ -670,6 +674,12 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   };
   constexpr int kCopies = 5;             // of a wavefront and tile
 
+  auto first_copies = [&]() __attribute__((always_inline)) {
+    __syncthreads();                     // (earlier readers of the LDS are done)
+    for (int i = 0; i < kStages - 1; ++i)
+      if (p.t0 + i < p.t1) copy_tile(p.t0 + i);
+  };
+  first_copies();
   // Q^T operand: step 2 cc + e of the d axis holds d = 32 cc + 16 h + 8 e + [0, 8)
   vec8 q[8];
   {
@@ -683,9 +693,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   if constexpr (kCoded) cq = code_q(q);
   f32x16 o[4], s_a, s_b;
   const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = zero;
-  float m = -INFINITY, l = 0.f, mx = -INFINITY;
+  float m, l, mx;
 
   // LDS offsets of this lane's fragments within a stage, of half tile 0; half tile 1 lies two pages behind
   const int k_page = n >> 2 & 1, k_slot = (n >> 3) * 4 + (n & 3);
@@ -736,11 +744,6 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     }
   };
 
-  __syncthreads();                       // (earlier readers of the LDS are done)
-  for (int i = 0; i < kStages - 1; ++i)
-    if (p.t0 + i < p.t1) copy_tile(p.t0 + i);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
   // Tile t + 1 is there, for every wavefront, and none reads tile t - 1 any more.
   auto turn = [&](int t) __attribute__((always_inline)) {
     if (t + 2 < p.t1)
@@ -752,12 +755,14 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   };
 
   // s: scores of keys key0 .. key0 + 31, s_next: of the 32 behind them, whose codes are in kc
-  auto half_step = [&](int t, auto which, f32x16& s, f32x16& s_next) __attribute__((always_inline)) {
+  // kFixed: the rows' reference stays where the first half put it (see run)
+  auto half_step = [&](auto fixed, int t, auto which, f32x16& s, f32x16& s_next) __attribute__((always_inline)) {
+    constexpr bool kFixed = decltype(fixed)::value;
     constexpr int kHalf = decltype(which)::value;
     const int key0 = t * kBN + 32 * kHalf;
     const uint32_t stage = stage_at(t), next = stage_at(t + 1);   // (behind the last tile: stale, and not used)
     // the rows' reference moves when a maximum has risen by more than 2^8
-    if (__builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
+    if (!kFixed && __builtin_amdgcn_ballot_w64(mx > m + 8.f) != 0) {
       const float m_new = fmaxf(m, mx);
       const float f = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
@@ -765,7 +770,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] *= f;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = !kFixed && m == -INFINITY ? 0.f : m;
     const float vs = *reinterpret_cast<const float*>(lds + stage + vs_off + kHalf * 512);
     uint32_t pk[8];
     float e0, e1;
@@ -780,6 +785,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     };
     vec8 op;
     // ---- phase 1: words 0..3 (all) of P are made on the way
+    __builtin_amdgcn_s_setprio(0);
     constexpr int kEarly = kCoded ? 8 : 4;
     if constexpr (kCoded) {
       const int k_scale = __builtin_bit_cast(uint32_t, ks) >> 23;
@@ -823,6 +829,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       mend_v(key0);
     }
     // ---- phase 2: V's d blocks with keys 0..7 of the page, then with keys 8..15
+    __builtin_amdgcn_s_setprio(1);
     load_ks(next, kHalf);
     op = numbers<T>(vc[0][0], vc[0][1], vs);
     float x = -INFINITY;
@@ -840,7 +847,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
         // the half behind the next: of this tile's successor
         if constexpr (kHalf == 0) load_k(next, 0, u);
         else load_k(next, 1, u);
-      } else {
+      } else if (!kFixed) {
         x = max3(x, s_next[4 * (u - 4)], s_next[4 * (u - 4) + 1]);
         x = max3(x, s_next[4 * (u - 4) + 2], s_next[4 * (u - 4) + 3]);
       }
@@ -850,9 +857,23 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    mx = across(x);
+    if (!kFixed) mx = across(x);
   };
-  if (active && p.t0 < p.t1) {
+  // One pass over the piece.  Any reference gives the same O and sum as long as nothing leaves fp32's range, and in bf16
+  // P keeps that range: a reference that stays at the first half tile's maximum spares the others theirs, their
+  // comparison and the exchange between lanes, a seventh of the vector instructions.  The caller looks at the
+  // sums afterwards, and repeats the pass with a reference that moves where they left the safe range.
+  auto run = [&](bool may_fix) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = zero;
+    m = mx = -INFINITY;
+    l = 0.f;
+    if (!active || p.t0 >= p.t1) {
+      for (int t = p.t0; t < p.t1; ++t) turn(t);
+      return;
+    }
     const uint32_t stage = stage_at(p.t0);
     load_ks(stage, 0);
 #pragma unroll
@@ -874,12 +895,31 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     load_ks(stage, 1);
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) load_k(stage, 1, cc);
-    for (int t = p.t0; t < p.t1; ++t) {
-      half_step(t, std::integral_constant<int, 0>(), s_a, s_b);
-      half_step(t, std::integral_constant<int, 1>(), s_b, s_a);
+    auto loop = [&](auto fixed) __attribute__((always_inline)) {
+      for (int t = p.t0; t < p.t1; ++t) {
+        half_step(fixed, t, std::integral_constant<int, 0>(), s_a, s_b);
+        half_step(fixed, t, std::integral_constant<int, 1>(), s_b, s_a);
+      }
+    };
+    // (a row that sees no key of the first half has no reference there)
+    if (kCoded && may_fix && __builtin_amdgcn_ballot_w64(mx == -INFINITY) == 0) {
+      m = mx;
+      loop(std::true_type());
+    } else {
+      loop(std::false_type());
     }
-  } else {
-    for (int t = p.t0; t < p.t1; ++t) turn(t);
+  };
+  for (bool again = false;; again = true) {
+    run(!again);
+    if (!kCoded || again) break;
+    // A sum below 2^60 proves that no exponential was lost; an accumulator that is infinite or not a number shows here.
+    float ends = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ends = __builtin_fmaf(o[i][r], 0.f, ends);
+    if (!__syncthreads_or(!(l < 0x1p60f) || ends != 0.f)) break;
+    first_copies();
   }
   l += __shfl_xor(l, 32);
   if (row >= p.ntok * G) return;
@@ -989,15 +1029,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   if (hdr.magic != kPlanMagic || hdr.heads != a.hkv * 16 + G || hdr.batch != a.batch || hdr.total_q != a.total_q ||
       hdr.tile_rows != kRows)
     return;
-  const int64_t visits = hdr.visits, span = hdr.span;
+  const int64_t units = hdr.units, span = hdr.span;
   // neighbouring spans, which share K and V, on one XCD (workgroups go to the XCDs in turns)
   const int w = blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds;
   if (!kFewOnly && threadIdx.x == 0) a.merges[w].count = 0;
   int64_t at = w * span;
-  const int64_t end = min(at + span, visits * a.hkv);
+  const int64_t end = min(at + span, units * a.hkv);
   if (at >= end) return;
-  int hk = (int)(at / visits);
-  int64_t in_head = at - hk * visits;
+  int hk = (int)(at / units);
+  int64_t in_head = at - hk * units;
   // the sequence: the last s with cum[s] <= in_head (of equal ones the last, which is not empty)
   int s = 0;
   {
@@ -1011,7 +1051,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     }
     s = __builtin_amdgcn_readfirstlane(s);
   }
-  // the tile: the last i with visits_before(i) <= what is left
+  // the q tile: the last i with units_before(i) <= what is left
   int64_t tile = 0;
   {
     const int64_t left = in_head - a.cum[s];
@@ -1019,7 +1059,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     int64_t cnt = (q + tok - 1) / tok;
     while (cnt > 1) {
       const int64_t half = cnt / 2;
-      if (visits_before(a.seqs[s].begin, q, tok, tile + half) <= left) {
+      if (units_before(a.seqs[s].begin, q, tok, tile + half) <= left) {
         tile += half;
         cnt -= half;
       } else {
@@ -1033,9 +1073,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     const bool few = kFewOnly || tok == kFewRows / G;
     const int row0 = (int)tile * tok, ntok = min(tok, q - row0);
     const int planned = (int)tiles64((int64_t)b + row0 + ntok);     // KV tiles of this q tile, by the plan
-    const int64_t tile_at = hk * visits + a.cum[s] + visits_before(b, q, tok, tile);
-    const int t0 = (int)(at - tile_at), t1 = (int)min((int64_t)planned, t0 + (end - at));
-    if (t0 < 0 || t1 <= t0) return;     // (never of a plan: a workspace written over)
+    const int64_t tile_at = hk * units + a.cum[s] + units_before(b, q, tok, tile), first = tile_at + kTileCost;
+    const int64_t stop = min(first + planned, end);
+    const int t0 = (int)max(at - first, (int64_t)0), t1 = (int)max(stop - first, (int64_t)0);
+    if (at < tile_at || at >= first + planned) return;     // (never of a plan: a workspace written over)
     const int now = a.begin[s];
     Piece p;
     p.hk = hk;
@@ -1051,7 +1092,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     // what a table of the length that the plan saw cannot hold is not read
     const bool ok = a.verdict[s] == MC_OK && now >= 0 && p.last_entry < a.cu_pages[s + 1] - p.table_off;
     const bool whole = t0 == 0 && t1 == planned;
-    if (ok) {
+    if (ok && t0 < t1) {
       Target to;
       to.part = whole ? -1 : 2 * w + (t0 == 0 ? 1 : 0);
       if (few)
@@ -1059,7 +1100,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
       else if constexpr (!kFewOnly)
         tile_piece<T, G>(a, p, to, lds);
       if (!whole) {
-        const int w0 = (int)(tile_at / span), count = (int)((tile_at + planned - 1) / span) - w0 + 1;
+        const int w0 = (int)(first / span), count = (int)((first + planned - 1) / span) - w0 + 1;
         if (!few) {
           if (t0 == 0 && threadIdx.x == 0) a.merges[w] = MergeRec8{p.q_first, p.ntok, p.hk, count};
         } else {
@@ -1077,14 +1118,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
         }
       }
     }
-    at += t1 - t0;
+    at = stop;
     if ((tile + 1) * tok < q) {
       ++tile;
     } else {
       tile = 0;
       // the next sequence with new tokens, of this kv head or the next
       const int64_t done = a.cum[s + 1];
-      if (done == visits) {
+      if (done == units) {
         ++hk;
         s = 0;
         while (s + 1 < a.batch && a.cum[s + 1] == 0) ++s;

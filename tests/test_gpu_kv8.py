@@ -253,13 +253,34 @@ def test_attention(dtype, hq, hkv, begin, new):
 
 
 @BOTH
-@pytest.mark.parametrize("scale, spread", [(1.0, 0), (0.01, 0), (None, 3)])
+@pytest.mark.parametrize("scale, spread", [(1.0, 0), (0.01, 0), (None, 3), (12.0, 0)])
 def test_attention_of_other_scales(dtype, scale, spread):
-    """Scores of a standard deviation of 11 (rows whose maximum moves far), of 0.1, and of keys of many sizes."""
+    """Scores of a standard deviation of 11 (rows whose maximum moves far), of 0.1, of keys of many sizes, and of 140 (rows
+    whose later keys beat the first ones by more than 2^60 in the exponent)."""
     rng = np.random.default_rng(7)
-    c = Case(rng, dtype, 2, [700, 20], [3, 150])
+    c = Case(rng, dtype, 2, [700, 20, 1100], [3, 150, 40])
     c.fill(upto=c.begin + c.new, spread=spread)
     run_attention(c, 8, scale=scale)
+
+
+@BOTH
+@pytest.mark.parametrize("new", [1, 90])
+def test_queries_of_many_sizes(dtype, new):
+    """Numbers of a row of q from 2^-12 to 2^12 of each other, d by d, each d with keys of the other size; rows of zeros."""
+    rng = np.random.default_rng(23)
+    c = Case(rng, dtype, 2, [333], [new])
+    n = 333 + new
+    by = 2.0 ** rng.integers(-6, 7, 128)
+    k = torch.from_numpy(rng.normal(size=(n, 2, 128)) / by).to(TYPES[dtype]).view(torch.int16).numpy().view(np.uint16)
+    c.o.append(0, k, normal_bits(rng, (n, 2, 128), dtype), 0, c.tables[0])
+    c.upload()
+    c.args_begin, c.args_new = c.begin, c.new
+    c.batch()
+    x = rng.normal(size=(new, 8, 128)) * by
+    x[new // 2, 3] = 0.0
+    q = torch.from_numpy(x).to(TYPES[dtype]).view(torch.int16).numpy().view(np.uint16)
+    out, lse, _ = attend(c, dev(q).view(TYPES[dtype]), 8)
+    check_attention(c, q, 8, out, lse)
 
 
 @pytest.mark.parametrize("new", [[1, 4], [100, 40]])
