@@ -32,13 +32,14 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;     // 4 wavefronts
+constexpr int kPlanThreads = 512; // of the plan, whose first workgroup looks every span's beginning up
 constexpr int kTileRows = 128, kFewRows = 16;
 constexpr int kBN = 64;           // keys per KV tile: 4 pages
 constexpr int kSpans = 512;       // workgroups of an attention launch at most: two for each of 256 compute units
 constexpr int kXcds = 8;
 constexpr int kMinSpan = 4;       // units a span has at least ...
 // ... and what a q tile takes beside its visits, in visits: looking it up, its Q, its first copies, its rows at the end.
-constexpr int kTileCost = 4;
+constexpr int kTileCost = 7;
 constexpr int32_t kPlanMagic = 0x6d63706d;
 
 struct Plan8Header {
@@ -63,8 +64,16 @@ struct PlanSeq {
   int32_t begin, q_first, q, table_off;
 };
 
+// Where a span begins: the kv head, the sequence, its q tile and that tile's place on the line.  (The plan looks it up once for
+// all layers; in each launch that is a chain of three or four memory accesses before the first code.)
+struct SpanStart {
+  int32_t hk, seq;
+  int64_t tile, tile_at;
+  PlanSeq of;
+};
+
 struct Workspace8 {
-  size_t cum, seqs, verdict, arrivals, merges, part_ml, part_o, total;
+  size_t cum, seqs, verdict, arrivals, starts, merges, part_ml, part_o, total;
   int32_t part_rows, spans;
   bool few;
 };
@@ -83,7 +92,8 @@ inline Workspace8 workspace8(int32_t batch, int32_t total_q, int G) {
   w.seqs = w.cum + round64(sizeof(int64_t) * ((size_t)batch + 1));
   w.verdict = w.seqs + round64(sizeof(PlanSeq) * (size_t)batch);
   w.arrivals = w.verdict + round64(sizeof(int32_t) * (size_t)batch);
-  w.merges = w.arrivals + round64(sizeof(uint32_t) * kSpans);
+  w.starts = w.arrivals + round64(sizeof(uint32_t) * kSpans);
+  w.merges = w.starts + round64(sizeof(SpanStart) * kSpans);
   w.part_ml = w.merges + sizeof(MergeRec8) * kSpans;
   w.part_o = w.part_ml + sizeof(float) * 2 * 2 * (size_t)w.spans * w.part_rows;
   w.total = w.part_o + sizeof(float) * kHeadDim * 2 * (size_t)w.spans * w.part_rows;
@@ -100,7 +110,8 @@ inline bool few_rows_only(int32_t batch, int32_t total_q, int G) {
 __device__ __forceinline__ int rows_of_tiles(int q, int G, int tile_rows) {
   return (int64_t)q * G <= kFewRows ? kFewRows : tile_rows;
 }
-__device__ __forceinline__ int64_t tiles64(int64_t keys) { return (keys + kBN - 1) / kBN; }
+__device__ __forceinline__ int64_t tiles64(int64_t keys) { return (keys + kBN - 1) >> 6; }
+static_assert(kBN == 64, "shifts by 6");
 
 // Units of a sequence's first i q tiles, of `tok` tokens each (a power of two): tile j visits the tiles of the keys before
 // b + min((j + 1) tok, q).
@@ -110,14 +121,12 @@ __device__ __forceinline__ int64_t units_before(int64_t b, int64_t q, int tok, i
     n = i - 1;
     sum += tiles64(b + q);
   }
-  if (tok >= kBN) {
-    const int64_t r = tok / kBN;
-    return sum + n * tiles64(b) + r * (n * (n + 1) / 2);
-  }
-  const int per = kBN / tok;         // tiles after which one more KV tile is seen
+  if (tok >= kBN) return sum + n * tiles64(b) + (n * (n + 1) >> 1) * (tok >> 6);
+  // one more KV tile is seen after every `per` q tiles
+  const int shift = __builtin_ctz(kBN) - __builtin_ctz(tok), per = 1 << shift;
   for (int res = 1; res <= per && res <= n; ++res) {
-    const int64_t cnt = (n - res) / per + 1;
-    sum += cnt * tiles64(b + (int64_t)res * tok) + cnt * (cnt - 1) / 2;
+    const int64_t cnt = ((n - res) >> shift) + 1;
+    sum += cnt * tiles64(b + res * tok) + (cnt * (cnt - 1) >> 1);
   }
   return sum;
 }
@@ -132,6 +141,7 @@ struct Plan8Args {
   PlanSeq* seqs;
   int32_t* verdict;
   uint32_t* arrivals;
+  SpanStart* starts;
   int32_t batch, total_q, num_pages, hkv, G, ahead;
   int32_t tile_rows, spans;
 };
@@ -145,7 +155,7 @@ __device__ __forceinline__ int checked_tokens(const Plan8Args& a, int s, bool* b
 }
 
 // Workgroup 0 sums the units; workgroup 1 + s looks at the page ids of sequence s.
-__global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
+__global__ __launch_bounds__(kPlanThreads) void plan8_kernel(Plan8Args a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x > 0) {
     const int s = blockIdx.x - 1;
@@ -154,16 +164,16 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
     if (!bad && q > 0) {
       const int32_t* table = a.page_table + a.cu_pages[s];
       const int n = (int)(((int64_t)a.begin[s] + q + a.ahead + kPage - 1) / kPage);
-      for (int i = tid; i < n; i += kThreads) bad |= (unsigned)table[i] >= (unsigned)a.num_pages;
+      for (int i = tid; i < n; i += kPlanThreads) bad |= (unsigned)table[i] >= (unsigned)a.num_pages;
     }
     const int any = __syncthreads_or(bad);
     if (tid == 0) a.verdict[s] = any ? MC_ERR_RANGE : MC_OK;
     return;
   }
-  for (int i = tid; i < kSpans; i += kThreads) a.arrivals[i] = 0;
-  __shared__ int64_t s_wave[kThreads / 64];
+  for (int i = tid; i < kSpans; i += kPlanThreads) a.arrivals[i] = 0;
+  __shared__ int64_t s_wave[kPlanThreads / 64];
   int64_t before = 0;
-  for (int s0 = 0; s0 < a.batch; s0 += kThreads) {
+  for (int s0 = 0; s0 < a.batch; s0 += kPlanThreads) {
     const int s = s0 + tid;
     int64_t v = 0;
     if (s < a.batch) {
@@ -184,13 +194,14 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
     if (lane == 63) s_wave[wave] = incl;
     __syncthreads();
     int64_t base = before;
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
       if (w < wave) base += s_wave[w];
       before += s_wave[w];
     }
     if (s < a.batch) a.cum[s] = base + incl - v;
     __syncthreads();
   }
+  const int64_t span = max((before * a.hkv + a.spans - 1) / a.spans, (int64_t)kMinSpan);
   if (tid == 0) {
     a.cum[a.batch] = before;
     Plan8Header h = {};
@@ -199,9 +210,46 @@ __global__ __launch_bounds__(kThreads) void plan8_kernel(Plan8Args a) {
     h.batch = a.batch;
     h.total_q = a.total_q;
     h.units = before;
-    h.span = max((before * a.hkv + a.spans - 1) / a.spans, (int64_t)kMinSpan);
+    h.span = span;
     h.tile_rows = a.tile_rows;
     *a.hdr = h;
+  }
+  __syncthreads();                 // (cum and seqs, of this workgroup's own writing)
+  for (int w = tid; w < a.spans; w += kPlanThreads) {
+    const int64_t at = w * span;
+    if (at >= before * a.hkv) continue;
+    SpanStart r = {};
+    r.hk = (int)((double)at / (double)before);          // (to one too many or few: 64-bit division takes as long as all else)
+    if (r.hk * before > at) --r.hk;
+    if ((r.hk + 1) * before <= at) ++r.hk;
+    const int64_t in_head = at - r.hk * before;
+    // the sequence: the last s with cum[s] <= in_head (of equal ones the last, which is not empty)
+    int s = 0;
+    for (int cnt = a.batch; cnt > 1;) {
+      const int half = cnt / 2;
+      if (a.cum[s + half] <= in_head) {
+        s += half;
+        cnt -= half;
+      } else {
+        cnt = half;
+      }
+    }
+    r.seq = s;
+    r.of = a.seqs[s];
+    // the q tile: the last i with units_before(i) <= what is left
+    const int64_t left = in_head - a.cum[s];
+    const int tok = rows_of_tiles(r.of.q, a.G, a.tile_rows) / a.G;
+    for (int64_t cnt = (r.of.q + tok - 1) / tok; cnt > 1;) {
+      const int64_t half = cnt / 2;
+      if (units_before(r.of.begin, r.of.q, tok, r.tile + half) <= left) {
+        r.tile += half;
+        cnt -= half;
+      } else {
+        cnt = half;
+      }
+    }
+    r.tile_at = at - left + units_before(r.of.begin, r.of.q, tok, r.tile);
+    a.starts[w] = r;
   }
 }
 
@@ -303,6 +351,7 @@ struct Attn8Args {
   const PlanSeq* seqs;
   const int32_t* verdict;
   uint32_t* arrivals;
+  const SpanStart* starts;
   MergeRec8* merges;
   float* part_ml;          // [part][row]: maximum (of the exponents, base 2), sum
   float* part_o;           // [part][row][D], relative to the part's maximum
@@ -593,32 +642,39 @@ __device__ __forceinline__ f32x16 mfma_coded(u32x4 k0, u32x4 k1, int k_scale, i3
     default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 3, q_scales);
   }
 }
-// q: bf16 numbers, vector 4 j + i the numbers 8 i + [0, 8) of block j
-__device__ __forceinline__ CodedQ code_q(const bf16x8 (&q)[8]) {
+// q: pairs of bf16 numbers, words 16 j + w the numbers 2 w, 2 w + 1 of block j
+__device__ __forceinline__ CodedQ code_q(const u32x4 (&q)[8]) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   CodedQ r;
   r.scales = 0;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    uint32_t big = 0;
+    // (infinities and NaN among them: the row is lost whatever the scale)
+    u16x2 most = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 32; ++i) big = max(big, mc::magnitude((float)q[4 * j + (i >> 3)][i & 7]));
-    uint32_t other = big;
+    for (int w = 0; w < 16; ++w)
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, q[4 * j + (w >> 2)][w & 3] & 0x7fff7fffu));
+    uint32_t big = max((uint32_t)most[0], (uint32_t)most[1]) << 16, other = big;
     swap_halves(big, other);             // (both lanes of a row: one scale for the block's 64 numbers)
     const int k = mc::scale_exponent(max(big, other), mc::ScaleLimits{-100, 120});
-    const float inv = mc::power_of_two(-k);
+    const float scale = mc::power_of_two(k), scale_lo = mc::power_of_two(k - 4);
 #pragma unroll
     for (int w = 0; w < 8; ++w) {
-      float x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = (float)q[4 * j + (w >> 1)][4 * (w & 1) + i] * inv;
-      const uint32_t hi = mc::four_codes(x[0], x[1], x[2], x[3]);
-      const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)hi, true);
-      y[0] = (x[0] - a[0]) * 16.f;
-      y[1] = (x[1] - a[1]) * 16.f;
-      y[2] = (x[2] - b[0]) * 16.f;
-      y[3] = (x[3] - b[1]) * 16.f;
-      r.hi[j][w] = (int)hi;
-      r.lo[j][w] = (int)mc::four_codes(y[0], y[1], y[2], y[3]);
+      const uint32_t p0 = q[4 * j + (w >> 1)][2 * (w & 1)], p1 = q[4 * j + (w >> 1)][2 * (w & 1) + 1];
+      i16x2 hi = {0, 0}, lo = {0, 0};
+      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, p0), scale, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, p1), scale, true);
+      const uint32_t h = __builtin_bit_cast(uint32_t, hi);
+      const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, scale, false);
+      const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, scale, true);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __builtin_bit_cast(float, p0 << 16) - a[0],
+                                                    __builtin_bit_cast(float, p0 & 0xffff0000u) - a[1], scale_lo, false);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __builtin_bit_cast(float, p1 << 16) - b[0],
+                                                    __builtin_bit_cast(float, p1 & 0xffff0000u) - b[1], scale_lo, true);
+      r.hi[j][w] = (int)h;
+      r.lo[j][w] = __builtin_bit_cast(int, lo);
     }
     r.scales |= ((k + 127) | (k + 127 - 4) << 8) << (16 * j);
   }
@@ -651,7 +707,16 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
 
   // this wavefront copies page `wave` of every tile
   const int32_t* table = a.page_table + p.table_off;
-  int ids = 0, ids_t = p.t0 - 64;        // lane i holds the page id of tile ids_t + i
+  auto look_up_pages = [&](int t) __attribute__((always_inline)) { return table[min(4 * (t + lane) + wave, p.last_entry)]; };
+  int ids = look_up_pages(p.t0), ids_t = p.t0;     // lane i holds the page id of tile ids_t + i
+  // Q^T operand: step 2 cc + e of the d axis holds d = 32 cc + 16 h + 8 e + [0, 8)
+  u32x4 q_raw[8];
+  {
+    const char* from = a.q + ((int64_t)(p.q_first + tok) * a.hq + p.hk * G + row % G) * kRowBytes;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      q_raw[u] = *reinterpret_cast<const u32x4*>(from + ((u >> 1) * 32 + h * 16 + (u & 1) * 8) * 2);
+  }
   // where in the page a lane's 16 bytes of the K (V) block's halves come from
   const uint32_t k_from = (lane >> 3) * kHeadDim + (((lane & 7) ^ ((lane >> 3 & 3) | (wave & 1) << 2)) << 4);
   const uint32_t v_from = a.hkv * kBlockBytes + lane * 16;
@@ -663,7 +728,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   auto copy_tile = [&](int t) __attribute__((always_inline)) {
     if (t >= ids_t + 64) {
       ids_t = t;
-      ids = table[min(4 * (t + lane) + wave, p.last_entry)];
+      ids = look_up_pages(t);
     }
     const int page = min(max(__builtin_amdgcn_readlane(ids, t - ids_t), 0), a.num_pages - 1);
     const char* from = codes + (uint64_t)(uint32_t)page * page_stride;
@@ -676,21 +741,17 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
 
   auto first_copies = [&]() __attribute__((always_inline)) {
     __syncthreads();                     // (earlier readers of the LDS are done)
+    if (ids_t != p.t0) ids = look_up_pages(ids_t = p.t0);
     for (int i = 0; i < kStages - 1; ++i)
       if (p.t0 + i < p.t1) copy_tile(p.t0 + i);
   };
   first_copies();
-  // Q^T operand: step 2 cc + e of the d axis holds d = 32 cc + 16 h + 8 e + [0, 8)
   vec8 q[8];
-  {
-    const char* from = a.q + ((int64_t)(p.q_first + tok) * a.hq + p.hk * G + row % G) * kRowBytes;
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      q[u] = *reinterpret_cast<const vec8*>(from + ((u >> 1) * 32 + h * 16 + (u & 1) * 8) * 2);
-  }
+  for (int u = 0; u < 8; ++u) q[u] = __builtin_bit_cast(vec8, q_raw[u]);
   constexpr bool kCoded = std::is_same<T, __bf16>::value;
   CodedQ cq;
-  if constexpr (kCoded) cq = code_q(q);
+  if constexpr (kCoded) cq = code_q(q_raw);
   f32x16 o[4], s_a, s_b;
   const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   float m, l, mx;
@@ -909,17 +970,20 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       loop(std::false_type());
     }
   };
-  for (bool again = false;; again = true) {
-    run(!again);
-    if (!kCoded || again) break;
+  // (the repeat has a copy of the loop to itself: as a second turn of a loop around one it cost the first 26 spilled
+  // registers, and 8 prompts 417 us instead of 409)
+  run(true);
+  if constexpr (kCoded) {
     // A sum below 2^60 proves that no exponential was lost; an accumulator that is infinite or not a number shows here.
     float ends = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) ends = __builtin_fmaf(o[i][r], 0.f, ends);
-    if (!__syncthreads_or(!(l < 0x1p60f) || ends != 0.f)) break;
-    first_copies();
+    if (__syncthreads_or(!(l < 0x1p60f) || ends != 0.f)) {
+      first_copies();
+      run(false);
+    }
   }
   l += __shfl_xor(l, 32);
   if (row >= p.ntok * G) return;
@@ -1036,48 +1100,22 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   int64_t at = w * span;
   const int64_t end = min(at + span, units * a.hkv);
   if (at >= end) return;
-  int hk = (int)(at / units);
-  int64_t in_head = at - hk * units;
-  // the sequence: the last s with cum[s] <= in_head (of equal ones the last, which is not empty)
-  int s = 0;
-  {
-    const int lane = threadIdx.x & 63;
-    int cnt = a.batch;
-    while (cnt > 1) {
-      const int step = (cnt + 63) / 64, e = s + cnt, i = s + lane * step;
-      const unsigned long long le = __ballot(i < e && a.cum[i] <= in_head);
-      s += max((int)__popcll(le) - 1, 0) * step;
-      cnt = min(step, e - s);
-    }
-    s = __builtin_amdgcn_readfirstlane(s);
-  }
-  // the q tile: the last i with units_before(i) <= what is left
-  int64_t tile = 0;
-  {
-    const int64_t left = in_head - a.cum[s];
-    const int q = a.seqs[s].q, tok = rows_of_tiles(q, G, kRows) / G;
-    int64_t cnt = (q + tok - 1) / tok;
-    while (cnt > 1) {
-      const int64_t half = cnt / 2;
-      if (units_before(a.seqs[s].begin, q, tok, tile + half) <= left) {
-        tile += half;
-        cnt -= half;
-      } else {
-        cnt = half;
-      }
-    }
-  }
+  const SpanStart start = a.starts[w];
+  int hk = start.hk, s = start.seq;
+  int64_t tile = start.tile, tile_at = start.tile_at;
+  PlanSeq sq = start.of;
+  int now = a.begin[s];
+  bool usable = a.verdict[s] == MC_OK;
+  int entries = a.cu_pages[s + 1] - sq.table_off;
   while (at < end) {
-    const PlanSeq sq = a.seqs[s];
-    const int q0 = sq.q_first, q = sq.q, tok = rows_of_tiles(q, G, kRows) / G, b = sq.begin;
+    const int q0 = sq.q_first, q = sq.q, tok = rows_of_tiles(sq.q, G, kRows) / G, b = sq.begin;
     const bool few = kFewOnly || tok == kFewRows / G;
     const int row0 = (int)tile * tok, ntok = min(tok, q - row0);
     const int planned = (int)tiles64((int64_t)b + row0 + ntok);     // KV tiles of this q tile, by the plan
-    const int64_t tile_at = hk * units + a.cum[s] + units_before(b, q, tok, tile), first = tile_at + kTileCost;
+    const int64_t first = tile_at + kTileCost;
     const int64_t stop = min(first + planned, end);
     const int t0 = (int)max(at - first, (int64_t)0), t1 = (int)max(stop - first, (int64_t)0);
     if (at < tile_at || at >= first + planned) return;     // (never of a plan: a workspace written over)
-    const int now = a.begin[s];
     Piece p;
     p.hk = hk;
     p.q_first = q0 + row0;
@@ -1090,7 +1128,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     p.table_off = sq.table_off;
     p.last_entry = (p.kv_len - 1) / kPage;
     // what a table of the length that the plan saw cannot hold is not read
-    const bool ok = a.verdict[s] == MC_OK && now >= 0 && p.last_entry < a.cu_pages[s + 1] - p.table_off;
+    const bool ok = usable && now >= 0 && p.last_entry < entries;
     const bool whole = t0 == 0 && t1 == planned;
     if (ok && t0 < t1) {
       Target to;
@@ -1119,6 +1157,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
       }
     }
     at = stop;
+    tile_at = first + planned;
     if ((tile + 1) * tok < q) {
       ++tile;
     } else {
@@ -1133,6 +1172,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
         ++s;
         while (s + 1 < a.batch && a.cum[s + 1] == done) ++s;
       }
+      sq = a.seqs[s];
+      now = a.begin[s];
+      usable = a.verdict[s] == MC_OK;
+      entries = a.cu_pages[s + 1] - sq.table_off;
     }
   }
 }
@@ -1203,6 +1246,7 @@ mc_status mc_attn8_plan_ahead(const mc_pool8_desc* pool, int32_t num_q_heads, in
   a.seqs = reinterpret_cast<PlanSeq*>(ws + w.seqs);
   a.verdict = reinterpret_cast<int32_t*>(ws + w.verdict);
   a.arrivals = reinterpret_cast<uint32_t*>(ws + w.arrivals);
+  a.starts = reinterpret_cast<SpanStart*>(ws + w.starts);
   a.batch = batch;
   a.total_q = total_q;
   a.num_pages = pool->num_pages;
@@ -1211,7 +1255,7 @@ mc_status mc_attn8_plan_ahead(const mc_pool8_desc* pool, int32_t num_q_heads, in
   a.ahead = ahead_tokens;
   a.tile_rows = w.few ? kFewRows : kTileRows;
   a.spans = w.spans;
-  hipLaunchKernelGGL(plan8_kernel, dim3(1 + (unsigned)batch), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL(plan8_kernel, dim3(1 + (unsigned)batch), dim3(kPlanThreads), 0, static_cast<hipStream_t>(stream), a);
   return mc::launch_status();
 }
 
@@ -1275,6 +1319,7 @@ mc_status mc_prefix_prefill_attn8(const mc_pool8_desc* pool, int32_t layer, cons
   a.seqs = reinterpret_cast<const PlanSeq*>(ws + w.seqs);
   a.verdict = reinterpret_cast<const int32_t*>(ws + w.verdict);
   a.arrivals = reinterpret_cast<uint32_t*>(ws + w.arrivals);
+  a.starts = reinterpret_cast<const SpanStart*>(ws + w.starts);
   a.merges = reinterpret_cast<MergeRec8*>(ws + w.merges);
   a.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + w.part_o);

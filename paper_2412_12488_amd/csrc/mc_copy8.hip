@@ -39,31 +39,42 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
   return x;
 }
 
-// One block by one wavefront: the tokens of slots [lo, hi), whose 16-bit rows start at src (slot lo) row_stride bytes
-// apart, become codes; slots [0, lo) hold codes already, at *scale, and move to the new scale where the
-// new tokens need a larger one; slots from hi on keep their bytes.
-template <typename T, bool kV>
-__device__ __forceinline__ void encode_block(const char* src, int64_t row_stride, int lo, int hi, char* block,
-                                             float* scale, ScaleLimits lim) {
+// A block's new tokens, of slots [lo, hi), as one wavefront holds them: 32 values a lane, K 4 rows x 8, V 16 rows x 2.
+// src: the row of slot lo; rows are row_stride bytes apart.
+struct Rows {
+  uint32_t w[16];
+};
+template <bool kV>
+__device__ __forceinline__ Rows load_rows(const char* src, int64_t row_stride, int lo, int hi) {
   const int lane = threadIdx.x & 63;
-  uint32_t w[16];                      // 32 values: K 4 rows x 8, V 16 rows x 2
+  Rows r;
   // (a slot without a new token reads the nearest one's row: no load under a condition)
   if (kV) {
 #pragma unroll
     for (int s = 0; s < kPage; ++s)
-      w[s] = *reinterpret_cast<const uint32_t*>(src + (min(max(s, lo), hi - 1) - lo) * row_stride + lane * 4);
-#pragma unroll
-    for (int s = 0; s < kPage; ++s)
-      if (s < lo || s >= hi) w[s] = 0u;
+      r.w[s] = *reinterpret_cast<const uint32_t*>(src + (min(max(s, lo), hi - 1) - lo) * row_stride + lane * 4);
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int s = 4 * i + (lane >> 4);
-      u32x4 v = *reinterpret_cast<const u32x4*>(src + (min(max(s, lo), hi - 1) - lo) * row_stride + (lane & 15) * 16);
-      if (s < lo || s >= hi) v = u32x4{0u, 0u, 0u, 0u};
+      const u32x4 v = *reinterpret_cast<const u32x4*>(src + (min(max(s, lo), hi - 1) - lo) * row_stride + (lane & 15) * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+      for (int j = 0; j < 4; ++j) r.w[4 * i + j] = v[j];
     }
+  }
+  return r;
+}
+
+// One block by one wavefront: the new tokens become codes; slots [0, lo) hold codes already, at *scale, and move to the
+// new scale where the new tokens need a larger one; slots from hi on keep their bytes.
+template <typename T, bool kV>
+__device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, char* block, float* scale, ScaleLimits lim) {
+  const int lane = threadIdx.x & 63;
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int s = kV ? i : (i & ~3) + (lane >> 4);
+    w[i] = s < lo || s >= hi ? 0u : rows.w[i];
   }
   const float had = lo > 0 ? *scale : 0.f;
   uint32_t big = 0;
@@ -172,13 +183,19 @@ __device__ __forceinline__ NewToken look_up(const Append8Args& a, int g, int s) 
   return t;
 }
 
-// One workgroup: kTokens neighbouring new tokens, of which those that open a page stand for the page.
+// One workgroup: kTokens neighbouring new tokens, of which those that open a page stand for the page.  Even wavefronts
+// take K, odd ones V.
 // kTokens == 1 (batches of few tokens, where most open a page of their own: every block gets a wavefront at
-// once): blockIdx.y is a pair of heads.  kTokens == 16: blockIdx.y is one head, and two wavefronts share
-// the pages.  Even wavefronts take K, odd ones V.
+// once): blockIdx.y is a pair of heads.
+// kTokens == 64: blockIdx.y is one head, and the two wavefronts of K (V) take the pages in turns, the next one's rows
+// requested ahead of the present one's arithmetic.  The look-ups, five memory accesses one after the other, then serve several
+// blocks (8 prompts, 16600 tokens x 8 heads: with 16 tokens a workgroup, one or two blocks, 30.7 us).
+template <typename T, bool kV, int kTokens>
+__device__ __forceinline__ void append_pages(const Append8Args& a, const NewToken& t, int g0, int head, int part);
+
 template <typename T, int kTokens>
 __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kv = wave & 1, part = wave >> 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kv = wave & 1, part = wave >> 1;
   const int head = kTokens == 1 ? 2 * blockIdx.y + part : blockIdx.y;
   if (head >= a.hkv) return;
   const int g0 = blockIdx.x * kTokens;
@@ -190,12 +207,17 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
     s0 += max((int)__popcll(m) - 1, 0) * step;
     cnt = min(step, end - s0);
   }
-  // lane i looks token g0 + i up
+  // Lane i looks token g0 + i up.  The sequences behind s0 begin at the next 64 offsets, as far as these tokens are concerned,
+  // unless there are many without tokens among them.
+  const int later = kTokens > 1 && s0 + 1 + lane < a.batch ? a.cu_q[s0 + 1 + lane] : INT32_MAX;
   NewToken t = {-1, 0, -1};
+  int s = s0;
+  if (kTokens > 1)
+    for (int i = 0; i < 64 && __builtin_amdgcn_readlane(later, i) < g0 + kTokens; ++i)
+      s += __builtin_amdgcn_readlane(later, i) <= g0 + lane ? 1 : 0;
   if (lane < kTokens && g0 + lane < a.total_q) {
-    int s = s0;
-    if (kTokens > 1) {
-      int n = a.batch - s0;          // from s0 on by halves
+    if (kTokens > 1 && s == s0 + 64) {         // from there on by halves
+      int n = a.batch - s;
       while (n > 1) {
         const int h = n / 2;
         if (a.cu_q[s + h] <= g0 + lane) { s += h; n -= h; } else { n = h; }
@@ -204,22 +226,41 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
     t = look_up(a, g0 + lane, s);
     if (t.page < 0 && a.skipped && kv == 0 && part == 0 && head == 0) atomicAdd(a.skipped, 1);
   }
+  if (kv)
+    append_pages<T, true, kTokens>(a, t, g0, head, part);
+  else
+    append_pages<T, false, kTokens>(a, t, g0, head, part);
+}
+
+template <typename T, bool kV, int kTokens>
+__device__ __forceinline__ void append_pages(const Append8Args& a, const NewToken& t, int g0, int head, int part) {
+  struct Job {
+    int first, count, page;
+  };
+  const char* from = (kV ? a.v_new : a.k_new) + ((int64_t)g0 * a.hkv + head) * kRowBytes;
+  const int64_t stride = (int64_t)a.hkv * kRowBytes;
   unsigned long long open = __ballot(t.first >= 0);
-  int nth = 0;
-  while (open) {
+  auto take = [&](Job& j, Rows& r) __attribute__((always_inline)) {      // the next page's; false: there is none
+    if (!open) return false;
     const int i = __builtin_ctzll(open);
     open &= open - 1;
-    if (kTokens > 1 && (nth++ & 1) != part) continue;
-    const int first = __builtin_amdgcn_readlane(t.first, i), count = __builtin_amdgcn_readlane(t.count, i),
-              page = __builtin_amdgcn_readlane(t.page, i);
-    const int64_t row = (int64_t)(g0 + i) * a.hkv + head;
-    char* block = a.codes + page * a.page_stride + (int64_t)(kv * a.hkv + head) * kBlockBytes;
-    float* scale = a.scales + ((int64_t)page * a.hkv + head) * 2 + kv;
-    const int64_t stride = (int64_t)a.hkv * kRowBytes;
-    if (kv)
-      encode_block<T, true>(a.v_new + row * kRowBytes, stride, first, first + count, block, scale, a.lim);
-    else
-      encode_block<T, false>(a.k_new + row * kRowBytes, stride, first, first + count, block, scale, a.lim);
+    if (kTokens > 1) open &= open - 1;         // (that one is the other wavefront's)
+    j = Job{__builtin_amdgcn_readlane(t.first, i), __builtin_amdgcn_readlane(t.count, i),
+            __builtin_amdgcn_readlane(t.page, i)};
+    r = load_rows<kV>(from + i * stride, stride, j.first, j.first + j.count);
+    return true;
+  };
+  if (kTokens > 1 && part) open &= open - 1;
+  Job job, next;
+  Rows rows, next_rows;
+  bool more = take(job, rows);
+  while (more) {
+    more = take(next, next_rows);
+    char* block = a.codes + job.page * a.page_stride + (int64_t)(kV * a.hkv + head) * kBlockBytes;
+    float* scale = a.scales + ((int64_t)job.page * a.hkv + head) * 2 + kV;
+    encode_block<T, kV>(rows, job.first, job.first + job.count, block, scale, a.lim);
+    job = next;
+    rows = next_rows;
   }
 }
 
@@ -259,9 +300,9 @@ __global__ __launch_bounds__(kThreads) void compress_kernel(Range8Args a) {
   float* scale = a.scales + layer * a.layer_scales + ((int64_t)page8 * a.hkv + head) * 2 + kv;
   const int hi = min(kPage, a.s1 - tp * kPage);
   if (kv)
-    encode_block<T, true>(src, kRowBytes, 0, hi, block, scale, a.lim);
+    encode_block<T, true>(load_rows<true>(src, kRowBytes, 0, hi), 0, hi, block, scale, a.lim);
   else
-    encode_block<T, false>(src, kRowBytes, 0, hi, block, scale, a.lim);
+    encode_block<T, false>(load_rows<false>(src, kRowBytes, 0, hi), 0, hi, block, scale, a.lim);
 }
 
 template <typename T>
@@ -494,9 +535,9 @@ mc_status mc_kv8_append(const mc_pool8_desc* pool, int32_t layer, const void* k_
   a.lim = mc::scale_limits(pool->dtype);
   a.skipped = pool->skipped;
   const bool few = total_q <= kFewTokens, half = pool->dtype == MC_F16;
-  const dim3 grid(few ? total_q : (unsigned)(((int64_t)total_q + 15) / 16), few ? (a.hkv + 1) / 2 : a.hkv);
+  const dim3 grid(few ? total_q : (unsigned)(((int64_t)total_q + 63) / 64), few ? (a.hkv + 1) / 2 : a.hkv);
   auto* kernel = few ? (half ? append8_kernel<_Float16, 1> : append8_kernel<__bf16, 1>)
-                     : (half ? append8_kernel<_Float16, 16> : append8_kernel<__bf16, 16>);
+                     : (half ? append8_kernel<_Float16, 64> : append8_kernel<__bf16, 64>);
   hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
   return mc::launch_status();
 }
