@@ -920,10 +920,12 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     }
     if (!kFixed) mx = across(x);
   };
-  // One pass over the piece.  Any reference gives the same O and sum as long as nothing leaves fp32's range, and in bf16
-  // P keeps that range: a reference that stays at the first half tile's maximum spares the others theirs, their
-  // comparison and the exchange between lanes, a seventh of the vector instructions.  The caller looks at the
-  // sums afterwards, and repeats the pass with a reference that moves where they left the safe range.
+  // One pass over the piece.  Any reference gives the same O and sum as long as nothing leaves P's range, and a reference
+  // that stays at the first half tile's maximum spares the others theirs, their comparison and the exchange
+  // between lanes, a seventh of the vector instructions.  The caller looks at the sums and accumulators afterwards, and
+  // repeats the pass with a reference that moves where something was lost.  (bf16 P has fp32's range; fp16 P ends at 2^16
+  // above the reference, beyond which it is an infinity, and has full precision down to 2^-14 below it, as
+  // with a reference that moves: that one lies at most 2^8 below the row's maximum.)
   auto run = [&](bool may_fix) __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -963,7 +965,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       }
     };
     // (a row that sees no key of the first half has no reference there)
-    if (kCoded && may_fix && __builtin_amdgcn_ballot_w64(mx == -INFINITY) == 0) {
+    if (may_fix && __builtin_amdgcn_ballot_w64(mx == -INFINITY) == 0) {
       m = mx;
       loop(std::true_type());
     } else {
@@ -973,7 +975,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   // (the repeat has a copy of the loop to itself: as a second turn of a loop around one it cost the first 26 spilled
   // registers, and 8 prompts 417 us instead of 409)
   run(true);
-  if constexpr (kCoded) {
+  {
     // A sum below 2^60 proves that no exponential was lost; an accumulator that is infinite or not a number shows here.
     float ends = 0.f;
 #pragma unroll

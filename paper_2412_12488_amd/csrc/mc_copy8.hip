@@ -32,11 +32,16 @@ __device__ __forceinline__ float high_half(uint32_t w) {
   return (float)__builtin_bit_cast(T, (uint16_t)(w >> 16));
 }
 
-// largest of all 64 lanes' values
+// largest of all 64 lanes' values, by data-parallel moves (rows of 16 lanes, then the rows' last ones)
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
-  return x;
+  auto step = [&](uint32_t y) __attribute__((always_inline)) { x = max(x, y); };
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));   // row_shr:1
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));   // row_bcast:15
+  step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));   // row_bcast:31
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 // A block's new tokens, of slots [lo, hi), as one wavefront holds them: 32 values a lane, K 4 rows x 8, V 16 rows x 2.
@@ -77,6 +82,13 @@ __device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, c
     w[i] = s < lo || s >= hi ? 0u : rows.w[i];
   }
   const float had = lo > 0 ? *scale : 0.f;
+  // of a V block, this lane's columns 2 lane and 2 lane + 1: 16 codes each, requested ahead of the arithmetic
+  u32x4* columns = reinterpret_cast<u32x4*>(block + lane * 32);
+  u32x4 a = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u};
+  if (kV && (lo > 0 || hi < kPage)) {
+    a = columns[0];
+    b = columns[1];
+  }
   uint32_t big = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i)
@@ -90,13 +102,6 @@ __device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, c
   }
   const float inv = mc::power_of_two(-k), most = k == lim.hi ? 240.f : 448.f;
   if (kV) {
-    // columns 2 lane and 2 lane + 1: 16 codes each
-    u32x4* to = reinterpret_cast<u32x4*>(block + lane * 32);
-    u32x4 a = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u};
-    if (lo > 0 || hi < kPage) {
-      a = to[0];
-      b = to[1];
-    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float x[4], y[4];
@@ -119,8 +124,8 @@ __device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, c
       a[j] = (na & fresh) | (oa & ~fresh);
       b[j] = (nb & fresh) | (ob & ~fresh);
     }
-    to[0] = a;
-    to[1] = b;
+    columns[0] = a;
+    columns[1] = b;
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
