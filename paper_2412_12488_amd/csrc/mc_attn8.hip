@@ -3,7 +3,7 @@
 // Work
 //   * A q tile is 128 rows (TOK = 128 / G tokens x the G query heads of one kv head) of one sequence, or all of its
 //     rows where those are at most 16 (decode steps).  A tile walks the 64-key KV tiles that its rows may see.
-//   * All visits of KV tiles by q tiles, kv head after kv head, form one line, each q tile's behind kTileCost units that
+//   * All visits of KV tiles by q tiles, kv head after kv head, form one line of units, each q tile's behind some that
 //     stand for what it takes beside them; plan8_kernel writes down how many units lie before each
 //     sequence, and the attention launch cuts the line into as many equal spans as workgroups run at a time.  A span is any mixture of whole q tiles and parts of some; a part's rows (O, maximum, sum)
 //     go to the workspace, and the last workgroup to finish a part of a q tile combines them, in their order.
@@ -37,8 +37,9 @@ constexpr int kTileRows = 128, kFewRows = 16;
 constexpr int kBN = 64;           // keys per KV tile: 4 pages
 constexpr int kSpans = 512;       // workgroups of an attention launch at most: two for each of 256 compute units
 constexpr int kXcds = 8;
-constexpr int kMinSpan = 4;       // units a span has at least ...
+constexpr int kMinSpan = 4;       // units a span has at least (no fewer than a visit's) ...
 // ... and what a q tile takes beside its visits, in visits: looking it up, its Q, its first copies, its rows at the end.
+// (8 prompts of 1024..4096 tokens, with 2 / 4 / 7: 457 / 430 / 407 us; 8 decode rows, a layer, 4 / 7: 20.7 / 19.7.)
 constexpr int kTileCost = 7;
 constexpr int32_t kPlanMagic = 0x6d63706d;
 
@@ -110,12 +111,16 @@ inline bool few_rows_only(int32_t batch, int32_t total_q, int G) {
 __device__ __forceinline__ int rows_of_tiles(int q, int G, int tile_rows) {
   return (int64_t)q * G <= kFewRows ? kFewRows : tile_rows;
 }
+// A visit by a q tile of 128 rows takes a workgroup about 1.5 us, one by a tile of few rows, which its wavefronts share,
+// 0.6: two units and one.  (24 decode rows of 700..2500 keys beside a range of 1066 tokens, 64 / 8 heads, fp16: one unit each
+// 94 us, so 78.)
+__device__ __forceinline__ int unit_shift(int rows) { return rows == kFewRows ? 0 : 1; }
 __device__ __forceinline__ int64_t tiles64(int64_t keys) { return (keys + kBN - 1) >> 6; }
 static_assert(kBN == 64, "shifts by 6");
 
-// Units of a sequence's first i q tiles, of `tok` tokens each (a power of two): tile j visits the tiles of the keys before
-// b + min((j + 1) tok, q).
-__device__ __forceinline__ int64_t units_before(int64_t b, int64_t q, int tok, int64_t i) {
+// Visits, and kTileCost for each tile, of a sequence's first i q tiles, of `tok` tokens each (a power of two): tile j visits
+// the tiles of the keys before b + min((j + 1) tok, q).
+__device__ __forceinline__ int64_t visits_before(int64_t b, int64_t q, int tok, int64_t i) {
   int64_t n = i, sum = i * kTileCost;
   if (i * tok > q) {                 // the last tile is short
     n = i - 1;
@@ -129,6 +134,10 @@ __device__ __forceinline__ int64_t units_before(int64_t b, int64_t q, int tok, i
     sum += cnt * tiles64(b + res * tok) + (cnt * (cnt - 1) >> 1);
   }
   return sum;
+}
+
+__device__ __forceinline__ int64_t units_before(const PlanSeq& s, int G, int rows, int64_t i) {
+  return visits_before(s.begin, s.q, rows / G, i) << unit_shift(rows);
 }
 
 struct Plan8Args {
@@ -179,11 +188,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan8_kernel(Plan8Args a) {
     if (s < a.batch) {
       bool bad;
       const int q = checked_tokens(a, s, &bad);
+      const PlanSeq of = {a.begin[s], a.cu_q[s], q, a.cu_pages[s]};
       if (q > 0) {
-        const int tok = rows_of_tiles(q, a.G, a.tile_rows) / a.G;
-        v = units_before(a.begin[s], q, tok, (q + tok - 1) / tok);
+        const int rows = rows_of_tiles(q, a.G, a.tile_rows), tok = rows / a.G;
+        v = units_before(of, a.G, rows, (q + tok - 1) / tok);
       }
-      a.seqs[s] = PlanSeq{a.begin[s], a.cu_q[s], q, a.cu_pages[s]};
+      a.seqs[s] = of;
     }
     int64_t incl = v;
 #pragma unroll
@@ -238,17 +248,17 @@ __global__ __launch_bounds__(kPlanThreads) void plan8_kernel(Plan8Args a) {
     r.of = a.seqs[s];
     // the q tile: the last i with units_before(i) <= what is left
     const int64_t left = in_head - a.cum[s];
-    const int tok = rows_of_tiles(r.of.q, a.G, a.tile_rows) / a.G;
+    const int rows = rows_of_tiles(r.of.q, a.G, a.tile_rows), tok = rows / a.G;
     for (int64_t cnt = (r.of.q + tok - 1) / tok; cnt > 1;) {
       const int64_t half = cnt / 2;
-      if (units_before(r.of.begin, r.of.q, tok, r.tile + half) <= left) {
+      if (units_before(r.of, a.G, rows, r.tile + half) <= left) {
         r.tile += half;
         cnt -= half;
       } else {
         cnt = half;
       }
     }
-    r.tile_at = at - left + units_before(r.of.begin, r.of.q, tok, r.tile);
+    r.tile_at = at - left + units_before(r.of, a.G, rows, r.tile);
     a.starts[w] = r;
   }
 }
@@ -1110,14 +1120,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   bool usable = a.verdict[s] == MC_OK;
   int entries = a.cu_pages[s + 1] - sq.table_off;
   while (at < end) {
-    const int q0 = sq.q_first, q = sq.q, tok = rows_of_tiles(sq.q, G, kRows) / G, b = sq.begin;
-    const bool few = kFewOnly || tok == kFewRows / G;
+    const int q0 = sq.q_first, q = sq.q, rows = rows_of_tiles(q, G, kRows), tok = rows / G, b = sq.begin;
+    const bool few = kFewOnly || rows == kFewRows;
+    const int shift = kFewOnly ? 0 : unit_shift(rows), weight = 1 << shift;
     const int row0 = (int)tile * tok, ntok = min(tok, q - row0);
     const int planned = (int)tiles64((int64_t)b + row0 + ntok);     // KV tiles of this q tile, by the plan
-    const int64_t first = tile_at + kTileCost;
-    const int64_t stop = min(first + planned, end);
-    const int t0 = (int)max(at - first, (int64_t)0), t1 = (int)max(stop - first, (int64_t)0);
-    if (at < tile_at || at >= first + planned) return;     // (never of a plan: a workspace written over)
+    // the visits whose first unit lies in this span (every span has at least kMinSpan units, so a visit's beginning)
+    const int64_t first = tile_at + (kTileCost << shift), tile_end = first + ((int64_t)planned << shift);
+    const int64_t stop = min(tile_end, end);
+    const int t0 = (int)(max(at - first + weight - 1, (int64_t)0) >> shift), t1 = (int)(max(stop - first + weight - 1, (int64_t)0) >> shift);
+    if (at < tile_at || at >= tile_end) return;     // (never of a plan: a workspace written over)
     Piece p;
     p.hk = hk;
     p.q_first = q0 + row0;
@@ -1140,7 +1152,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
       else if constexpr (!kFewOnly)
         tile_piece<T, G>(a, p, to, lds);
       if (!whole) {
-        const int w0 = (int)(first / span), count = (int)((first + planned - 1) / span) - w0 + 1;
+        const int w0 = (int)(first / span), count = (int)((tile_end - weight) / span) - w0 + 1;
         if (!few) {
           if (t0 == 0 && threadIdx.x == 0) a.merges[w] = MergeRec8{p.q_first, p.ntok, p.hk, count};
         } else {
@@ -1159,7 +1171,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
       }
     }
     at = stop;
-    tile_at = first + planned;
+    tile_at = tile_end;
     if ((tile + 1) * tok < q) {
       ++tile;
     } else {
