@@ -347,7 +347,7 @@ mc_status mc_kv_copy_page(const mc_pool_desc* pool, int32_t layer_begin, int32_t
  *
  * dtype is the 16-bit type of k_new, v_new, q and out.  codes is 16-byte, scales
  * 8-byte aligned.  Errors, streams, page tables, bounds checks and the counter of
- * what was skipped (mc_kv8_copy_check; a page counts once) are as above. */
+ * what was skipped (mc_kv8_copy_check: tokens of an append, else pages) are as above. */
 typedef struct {
   void* codes;
   float* scales;
@@ -385,7 +385,8 @@ mc_status mc_kv8_append(const mc_pool8_desc* pool, int32_t layer,
  * evenly among the workgroups that the GPU runs at a time; q tiles that it cuts are
  * combined before the call returns control of the stream.  Plan, workspace and
  * ahead_tokens follow the rules of mc_attn_plan and mc_attn_plan_ahead, and calls that
- * use one workspace must run one after the other; but a sequence whose offsets,
+ * use one workspace must run one after the other (its size: about 65 MiB at most and
+ * 28 bytes a sequence); but a sequence of more than 2^30 tokens, or whose offsets,
  * table or page ids are malformed is left out by itself (its out and lse rows are
  * not written) and the others are computed; mc_attn8_plan_check then returns
  * MC_ERR_RANGE.  The two kinds of plan are not interchangeable. */

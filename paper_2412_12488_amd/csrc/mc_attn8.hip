@@ -41,6 +41,7 @@ constexpr int kMinSpan = 4;       // units a span has at least (no fewer than a 
 // ... and what a q tile takes beside its visits, in visits: looking it up, its Q, its first copies, its rows at the end.
 // (8 prompts of 1024..4096 tokens, with 2 / 4 / 7: 457 / 430 / 407 us; 8 decode rows, a layer, 4 / 7: 20.7 / 19.7.)
 constexpr int kTileCost = 7;
+constexpr int kMostTokens = 1 << 30;   // of a sequence: positions stay far inside 32 bits
 constexpr int32_t kPlanMagic = 0x6d63706d;
 
 struct Plan8Header {
@@ -159,7 +160,7 @@ struct Plan8Args {
 __device__ __forceinline__ int checked_tokens(const Plan8Args& a, int s, bool* bad) {
   const int q0 = a.cu_q[s], q1 = a.cu_q[s + 1], b = a.begin[s], p0 = a.cu_pages[s], p1 = a.cu_pages[s + 1];
   *bad = q0 < 0 || q1 < q0 || q1 > a.total_q || b < 0 || p0 < 0 || p1 < p0 ||
-         (q1 > q0 && (int64_t)b + (q1 - q0) + a.ahead > ((int64_t)p1 - p0) * kPage);
+         (q1 > q0 && (int64_t)b + (q1 - q0) + a.ahead > min(((int64_t)p1 - p0) * kPage, (int64_t)kMostTokens));
   return *bad ? 0 : q1 - q0;
 }
 
@@ -432,6 +433,16 @@ struct Parts {
       : o(make_rsrc(a.part_o, 2ll * a.spans * a.part_rows * kHeadDim * 4)),
         ml(make_rsrc(a.part_ml, 2ll * a.spans * a.part_rows * 8)), rows(a.part_rows) {}
   __device__ __forceinline__ uint32_t at(int part, int row) const { return (uint32_t)(part * rows + row); }
+  // Rows of q tiles of 128 lie as a wavefront's registers do: vector (i, j) of all its lanes together.
+  __device__ __forceinline__ uint32_t vector_at(int part, int wave, int i, int j) const {
+    return (uint32_t)((((part * 4 + wave) * 4 + i) * 4 + j) * 64 + (threadIdx.x & 63)) * 16;
+  }
+  __device__ __forceinline__ void put_vector(uint32_t at, f32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), o, at, 0, kLaunchScope);
+  }
+  __device__ __forceinline__ f32x4 get_vector(uint32_t at) const {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(o, at, 0, kLaunchScope));
+  }
   template <int kScope>
   __device__ __forceinline__ void put(uint32_t i, int d, f32x4 v) const {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), o, (i * kHeadDim + d) * 4, 0, kScope);
@@ -628,6 +639,20 @@ __device__ __forceinline__ void few_rows_piece(const Attn8Args& a, const Piece& 
         u32x4{pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv),
               pack2<T>(acc[4] * inv, acc[5] * inv), pack2<T>(acc[6] * inv, acc[7] * inv)};
     if (d == 0) a.lse[at] = (mm + __builtin_amdgcn_logf(ll)) * 0.6931471805599453f;
+  }
+}
+
+// 32 d of a row, of which lane h (and its neighbour h ^ 1, 32 lanes away) holds 8 j + 4 h + [0, 4): 16 bytes a store, of j for
+// the lane with h = 0, of j + 1 for the other.
+template <typename T>
+__device__ __forceinline__ void store_block(char* to, int h, const f32x4 (&v)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; j += 2) {
+    uint32_t x0 = pack2<T>(v[j][0], v[j][1]), x1 = pack2<T>(v[j][2], v[j][3]);
+    uint32_t y0 = pack2<T>(v[j + 1][0], v[j + 1][1]), y1 = pack2<T>(v[j + 1][2], v[j + 1][3]);
+    swap_halves(x0, y0);
+    swap_halves(x1, y1);
+    *reinterpret_cast<u32x4*>(to + 16 * (j + h)) = u32x4{x0, x1, y0, y1};
   }
 }
 
@@ -998,101 +1023,138 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     }
   }
   l += __shfl_xor(l, 32);
-  if (row >= p.ntok * G) return;
   // lane: d = 32 i + 8 j + 4 h + [0, 4) of its row
   if (to.part >= 0) {
     const Parts parts(a);
-    const uint32_t at = parts.at(to.part, row);
+    if (!active) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        parts.put<kLaunchScope>(at, 32 * i + 8 * j + 4 * h,
-                                f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
-    if (h == 0) parts.put_ml<kLaunchScope>(at, m, l);
-  } else {
+        parts.put_vector(parts.vector_at(to.part, wave, i, j),
+                         f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]});
+    if (h == 0) parts.put_ml<kLaunchScope>(parts.at(to.part, row), m, l);
+  } else if (row < p.ntok * G) {
     const int64_t at = out_row<G>(a, p, row);
     const float inv = 1.f / l;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      f32x4 v[4];
 #pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        // the lane with h = 0 gets the row's 16 bytes of j, the other those of j + 1
-        uint32_t x0 = pack2<T>(o[i][4 * j] * inv, o[i][4 * j + 1] * inv), x1 = pack2<T>(o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv);
-        uint32_t y0 = pack2<T>(o[i][4 * j + 4] * inv, o[i][4 * j + 5] * inv), y1 = pack2<T>(o[i][4 * j + 6] * inv, o[i][4 * j + 7] * inv);
-        swap_halves(x0, y0);
-        swap_halves(x1, y1);
-        *reinterpret_cast<u32x4*>(a.out + at * kRowBytes + (32 * i + 8 * (j + h)) * 2) = u32x4{x0, x1, y0, y1};
-      }
+      for (int j = 0; j < 4; ++j) v[j] = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]} * inv;
+      store_block<T>(a.out + at * kRowBytes + 64 * i, h, v);
+    }
     if (h == 0) a.lse[at] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
 }
 
-// Rows first, first + step .. of a q tile whose parts spans w0 .. w0 + count - 1 have written, combined in their order:
-// 16 threads a row.  kAhead parts are requested at a time.
-template <typename T, int G, int kScope, int kAhead>
-__device__ __forceinline__ void combine(const Attn8Args& a, const Piece& p, int w0, int count, int first, int step) {
-  const Parts parts(a);
-  const int d = (threadIdx.x & 15) * 8;
-  for (int row = first + (threadIdx.x >> 4); row < p.ntok * G; row += step) {
-    // part 0 is the tile's beginning, at the end of its span; the others lie at the beginning of theirs
-    auto at = [&](int i) __attribute__((always_inline)) {
-      i = min(i, count - 1);
-      return parts.at(2 * (w0 + i) + (i == 0 ? 1 : 0), row);
-    };
-    float m = -INFINITY, l = 0.f;
-    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    for (int i0 = 0; i0 < count; i0 += kAhead) {
-      f32x2 ml[kAhead];
-      f32x4 o[kAhead][2];
+// Part i of a q tile that spans from w0 on have written: the tile's beginning lies at the end of its span, the others at the
+// beginning of theirs.
+__device__ __forceinline__ int part_of(int w0, int i) { return 2 * (w0 + i) + (i == 0 ? 1 : 0); }
+
+// The next kAhead parts' maxima and sums of a row, joined to what is there: factors of each part's O, and of the one so far.
+template <int kAhead>
+__device__ __forceinline__ float join(const f32x2 (&ml)[kAhead], int live, float& m, float& l, float (&f)[kAhead]) {
+  float mx = m;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) ml[i] = parts.get_ml<kScope>(at(i0 + i));
+  for (int i = 0; i < kAhead; ++i) mx = i < live ? fmaxf(mx, ml[i][0]) : mx;
+  const float ref = mx == -INFINITY ? 0.f : mx, f0 = __builtin_amdgcn_exp2f(m - ref);
+  m = mx;
+  l *= f0;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) o[i][j] = parts.get<kScope>(at(i0 + i), d + 4 * j);
-      float mx = m;
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) mx = fmaxf(mx, ml[i][0]);
-      const float ref = mx == -INFINITY ? 0.f : mx, f0 = __builtin_amdgcn_exp2f(m - ref);
-      l *= f0;
-      acc[0] *= f0;
-      acc[1] *= f0;
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const float f = i0 + i < count ? __builtin_amdgcn_exp2f(ml[i][0] - ref) : 0.f;
-        if (i0 + i < count) {
-          l += f * ml[i][1];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[j] += f * o[i][j];
-        }
-      }
-      m = mx;
-    }
-    const int64_t to = out_row<G>(a, p, row);
-    const float inv = 1.f / l;
-    *reinterpret_cast<u32x4*>(a.out + to * kRowBytes + d * 2) =
-        u32x4{pack2<T>(acc[0][0] * inv, acc[0][1] * inv), pack2<T>(acc[0][2] * inv, acc[0][3] * inv),
-              pack2<T>(acc[1][0] * inv, acc[1][1] * inv), pack2<T>(acc[1][2] * inv, acc[1][3] * inv)};
-    if (d == 0) a.lse[to] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  for (int i = 0; i < kAhead; ++i) {
+    f[i] = i < live ? __builtin_amdgcn_exp2f(ml[i][0] - ref) : 0.f;
+    l += i < live ? f[i] * ml[i][1] : 0.f;
   }
+  return f0;
 }
 
-// Cut q tiles of more than 16 rows, in a launch of its own: workgroup (span of a tile's beginning, 16 rows in turns).
+// The parts of a q tile of at most 16 rows, combined in their order: 16 threads a row.
+template <typename T, int G>
+__device__ __forceinline__ void combine_few(const Attn8Args& a, const Piece& p, int w0, int count) {
+  constexpr int kAhead = 8;
+  const Parts parts(a);
+  const int row = threadIdx.x >> 4, d = (threadIdx.x & 15) * 8;
+  if (row >= p.ntok * G) return;
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  for (int i0 = 0; i0 < count; i0 += kAhead) {
+    f32x2 ml[kAhead];
+    f32x4 o[kAhead][2];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ml[i] = parts.get_ml<kDeviceScope>(parts.at(part_of(w0, min(i0 + i, count - 1)), row));
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        o[i][j] = parts.get<kDeviceScope>(parts.at(part_of(w0, min(i0 + i, count - 1)), row), d + 4 * j);
+    float f[kAhead];
+    const float f0 = join(ml, count - i0, m, l, f);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      acc[j] *= f0;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i0 + i < count) acc[j] += f[i] * o[i][j];
+    }
+  }
+  const int64_t to = out_row<G>(a, p, row);
+  const float inv = 1.f / l;
+  *reinterpret_cast<u32x4*>(a.out + to * kRowBytes + d * 2) =
+      u32x4{pack2<T>(acc[0][0] * inv, acc[0][1] * inv), pack2<T>(acc[0][2] * inv, acc[0][3] * inv),
+            pack2<T>(acc[1][0] * inv, acc[1][1] * inv), pack2<T>(acc[1][2] * inv, acc[1][3] * inv)};
+  if (d == 0) a.lse[to] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// The parts of q tiles of 128 rows, in a launch of its own, bound by reading them: a workgroup takes 32 d of all rows of the
+// tile that begins in span w and goes on behind it, if there is one, on the XCD that wrote its first part.  (500 new
+// tokens over 4500, plan, attention and this: 66.5 us; on any XCD with 6 parts requested at a time instead of 4 64.1, on
+// this one 64.5, both 60.8.)
 constexpr int kMergeBlocks = 4;
 template <typename T, int G>
 __global__ __launch_bounds__(kThreads) void merge8_kernel(Attn8Args a) {
+  constexpr int kAhead = 6;
+  const int w = blockIdx.x % kXcds * (a.spans / kXcds) + blockIdx.x / kXcds / kMergeBlocks,
+            i32 = blockIdx.x / kXcds % kMergeBlocks;
+  const MergeRec8 r = a.merges[w];
   const Plan8Header hdr = *a.hdr;
   if (hdr.magic != kPlanMagic || hdr.heads != a.hkv * 16 + G || hdr.batch != a.batch || hdr.total_q != a.total_q)
     return;
-  const int w = blockIdx.x / kMergeBlocks;
-  const MergeRec8 r = a.merges[w];
   if (r.count < 2 || w + r.count > a.spans) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, row = wave * 32 + (lane & 31);
+  if (wave * 32 >= r.ntok * G) return;
+  const Parts parts(a);
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc[4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  for (int i0 = 0; i0 < r.count; i0 += kAhead) {
+    f32x2 ml[kAhead];
+    f32x4 o[kAhead][4];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ml[i] = parts.get_ml<kLaunchScope>(parts.at(part_of(w, min(i0 + i, r.count - 1)), row));
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        o[i][j] = parts.get_vector(parts.vector_at(part_of(w, min(i0 + i, r.count - 1)), wave, i32, j));
+    float f[kAhead];
+    const float f0 = join(ml, r.count - i0, m, l, f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      acc[j] *= f0;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i0 + i < r.count) acc[j] += f[i] * o[i][j];
+    }
+  }
+  if (row >= r.ntok * G) return;       // (both lanes of a row)
   Piece p = {};
   p.hk = r.hk;
   p.q_first = r.q_first;
-  p.ntok = r.ntok;
-  combine<T, G, kLaunchScope, 4>(a, p, w, r.count, blockIdx.x % kMergeBlocks * 16, 16 * kMergeBlocks);
+  const int64_t to = out_row<G>(a, p, row);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc[j] *= 1.f / l;
+  store_block<T>(a.out + to * kRowBytes + 64 * i32, h, acc);
+  if (i32 == 0 && h == 0) a.lse[to] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int G, bool kFewOnly>
@@ -1108,6 +1170,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
   const int64_t units = hdr.units, span = hdr.span;
   // neighbouring spans, which share K and V, on one XCD (workgroups go to the XCDs in turns)
   const int w = blockIdx.x % kXcds * (gridDim.x / kXcds) + blockIdx.x / kXcds;
+  static_assert(kSpans % kXcds == 0, "every span is some workgroup's");
   if (!kFewOnly && threadIdx.x == 0) a.merges[w].count = 0;
   int64_t at = w * span;
   const int64_t end = min(at + span, units * a.hkv);
@@ -1142,7 +1205,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
     p.table_off = sq.table_off;
     p.last_entry = (p.kv_len - 1) / kPage;
     // what a table of the length that the plan saw cannot hold is not read
-    const bool ok = usable && now >= 0 && p.last_entry < entries;
+    const bool ok = usable && now >= 0 && now <= kMostTokens && p.last_entry < entries;
     const bool whole = t0 == 0 && t1 == planned;
     if (ok && t0 < t1) {
       Target to;
@@ -1165,7 +1228,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn8_kernel(Attn8Args a) {
           if (s_last) {
             if (threadIdx.x == 0)      // for the next layer
               __hip_atomic_store(a.arrivals + w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            combine<T, G, kDeviceScope, 8>(a, p, w0, count, 0, kThreads / 16);
+            combine_few<T, G>(a, p, w0, count);
           }
         }
       }

@@ -362,6 +362,99 @@ def test_malformed_sequences_are_left_out_alone():
     check_attention(c, q[~lost], 8, out[~lost], lse[~lost])
 
 
+@BOTH
+def test_decode_batches_with_a_few_longer_ranges(dtype):
+    """No more new tokens than sequences, but some have several q tiles of 16 rows, and most none at all."""
+    rng = np.random.default_rng(24)
+    new = [0, 1, 0, 0, 9, 0, 0, 2, 0, 0, 0, 0]
+    c = Case(rng, dtype, 1, [5, 700, 0, 3, 1500, 0, 9, 64, 0, 1, 2, 3], new)
+    c.fill(upto=c.begin + c.new)
+    run_attention(c, 8)
+
+
+def test_many_sequences():
+    """1500 decode rows: several rounds of the plan's sums and of the append's look-ups."""
+    rng = np.random.default_rng(25)
+    B = 1500
+    c = Case(rng, kv8.BF16, 1, rng.integers(0, 40, B), [1] * B)
+    c.fill()
+    k, v = c.new_kv(spread=3)
+    mc.mc_kv8_append(c.desc, 0, dev(k), dev(v), *c.batch())
+    c.oracle_append(k, v)
+    c.same()
+    c.args_begin, c.args_new = c.begin, c.new
+    q = normal_bits(rng, (B, 4, 128), kv8.BF16)
+    out, lse, _ = attend(c, dev(q).view(torch.bfloat16), 4)
+    check_attention(c, q, 4, out, lse)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_pages_beyond_4_gib(new):
+    """The same sequence on low pages of a small pool and on pages past 2^32 bytes of a large one: the same bits."""
+    rng = np.random.default_rng(26)
+    heads, pages = 8, 140000
+    c = Case(rng, kv8.BF16, heads, [200], [new])
+    c.fill()
+    n = len(c.tables[0])
+    high = (pages - 1 - rng.permutation(3 * n)[:n]).astype(np.int32)
+    assert int(high.min()) * heads * 4096 > 1 << 32
+    codes = torch.empty(pages * heads * 4096, dtype=torch.uint8, device=DEV)
+    scales = torch.empty((pages, heads, 2), device=DEV)
+    big = mc.pool8_desc(codes, scales, 1, pages, heads, kv8.BF16)
+    buf = torch.empty(n * heads * 4104, dtype=torch.uint8, device=DEV)
+    low_t, high_t = dev(c.tables[0]), dev(high)
+    mc.mc_kv8_pack_range(c.desc, 0, 1, low_t, n, 0, 16 * n, buf)
+    mc.mc_kv8_unpack_range(big, 0, 1, high_t, n, 0, 16 * n, buf)
+    k, v = c.new_kv(spread=3)
+    q = dev(normal_bits(rng, (new, 32, 128), kv8.BF16)).view(torch.bfloat16)
+    args = c.batch()
+    mc.mc_kv8_append(c.desc, 0, dev(k), dev(v), *args)
+    low = attend(c, q, 32)
+    c.desc, c.args = big, args[:4] + [high_t] + args[5:]
+    mc.mc_kv8_append(big, 0, dev(k), dev(v), *c.args)
+    got = attend(c, q, 32)
+    assert torch.equal(low[0], got[0]) and torch.equal(low[1], got[1])
+    pool = torch.zeros((1, n, 2, heads, 16, 128), dtype=torch.bfloat16, device=DEV)
+    d16, ident = mc.pool_desc(pool, 1, n, heads, kv8.BF16), torch.arange(n, dtype=torch.int32, device=DEV)
+    back = torch.empty_like(buf)
+    mc.mc_kv8_pack_range(big, 0, 1, high_t, n, 0, 16 * n, buf)
+    mc.mc_kv8_restore_range(big, d16, 0, 1, high_t, n, ident, n, 0, 200 + new)
+    mc.mc_kv8_copy_page(big, 0, 1, int(high[0]), 3)
+    mc.mc_kv8_compress_range(d16, big, 0, 1, ident, n, high_t, n, 0, 200)
+    mc.mc_kv8_pack_range(big, 0, 1, high_t, n, 0, 16 * n, back)
+    page = heads * 4096
+    assert torch.equal(codes[3 * page:4 * page], buf[:page])
+    # whole pages of the 200 tokens: rounding what was rounded changes nothing (a scale may only be a smaller one)
+    at = codes.view(pages, 2, heads, 2048)[high_t.long()[:12]].view(torch.float8_e4m3fn).float()
+    x = at * scales[high_t.long()[:12]].transpose(1, 2)[..., None]
+    k16 = x[:, 0].view(12, heads, 16, 128)
+    assert torch.equal(k16, pool[0, :12, 0].float())
+
+
+def test_begins_out_of_range_are_left_out():
+    """At planning time, and when they change behind a plan."""
+    rng = np.random.default_rng(27)
+    c = Case(rng, kv8.BF16, 2, [40, 50], [1, 20])
+    c.fill(upto=c.begin + c.new)
+    q = dev(normal_bits(rng, (21, 8, 128), kv8.BF16)).view(torch.bfloat16)
+    for begin in ([40, 2 ** 31 - 1], [2 ** 31 - 1, -1], [-2 ** 31, 1 << 30]):
+        c.batch()
+        size = mc.mc_attn8_workspace_size(2, 21, 8, 2)
+        ws = torch.zeros(size, dtype=torch.uint8, device=DEV)
+        out = torch.full((21, 8, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((21, 8), float("nan"), device=DEV)
+        mc.mc_attn8_plan(c.desc, 8, *c.args, ws, size)
+        c.args[3] = dev(np.array(begin, np.int32))
+        mc.mc_prefix_prefill_attn8(c.desc, 0, q, 8, *c.args, 0.0, out, lse, ws, size)
+        good = begin[0] == 40
+        assert torch.isnan(lse[1:]).all() and torch.isnan(lse[0]).any() != good and torch.isnan(out[1:]).all()
+        mc.mc_attn8_plan(c.desc, 8, *c.args, ws, size)
+        with pytest.raises(mc.McError):
+            mc.mc_attn8_plan_check(ws)
+        mc.mc_prefix_prefill_attn8(c.desc, 0, q, 8, *c.args, 0.0, out, lse, ws, size)
+        assert torch.isnan(lse[1:]).all()
+
+
 def test_a_plan_of_another_batch_is_refused():
     rng = np.random.default_rng(11)
     c = Case(rng, kv8.BF16, 2, [40], [3])
