@@ -29,7 +29,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;     // 4 wavefronts
 constexpr int kPlanThreads = 512; // of the plan, whose first workgroup looks every span's beginning up
@@ -656,66 +655,6 @@ __device__ __forceinline__ void store_block(char* to, int h, const f32x4 (&v)[4]
   }
 }
 
-// ---- Q in codes -------------------------------------------------------------------------------
-// K Q^T can take K's codes as they are: the matrix instructions for scaled 8-bit numbers multiply a row by
-// a power of two of its own, which is what K's scales are.  A bf16 number has 8 significant bits and a code 4, so Q becomes
-// two rows of codes, hi and lo = the rest, lo at a 16th of hi's scale, with a scale per 64 numbers.  hi + lo is the number exactly
-// unless it is below 2^-14 of the largest of its 64; then it is off by at most 2^-23 of that, the size of
-// an fp32 rounding of it.  Two products of twice the rate take the matrix pipe's time of one in bf16, and K's
-// conversion, a fifth of the vector instructions of a half step, goes.  (fp16 numbers have 11 bits: three rows
-// would cost more than the conversion.)
-struct CodedQ {
-  i32x8 hi[2], lo[2];    // of d block j: 32 numbers of a lane, the other 32 in the row's other lane
-  int scales;            // exponents (E8M0): hi and lo of block 0, of block 1
-};
-__device__ __forceinline__ f32x16 mfma_coded(u32x4 k0, u32x4 k1, int k_scale, i32x8 q, int q_scales, int which, f32x16 c) {
-  const i32x8 k = {(int)k0[0], (int)k0[1], (int)k0[2], (int)k0[3], (int)k1[0], (int)k1[1], (int)k1[2], (int)k1[3]};
-  switch (which) {       // (the byte of q_scales is part of the instruction)
-    case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 0, q_scales);
-    case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 1, q_scales);
-    case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 2, q_scales);
-    default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, q, c, 0, 0, 0, k_scale, 3, q_scales);
-  }
-}
-// q: pairs of bf16 numbers, words 16 j + w the numbers 2 w, 2 w + 1 of block j
-__device__ __forceinline__ CodedQ code_q(const u32x4 (&q)[8]) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  CodedQ r;
-  r.scales = 0;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    // (infinities and NaN among them: the row is lost whatever the scale)
-    u16x2 most = {0, 0};
-#pragma unroll
-    for (int w = 0; w < 16; ++w)
-      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, q[4 * j + (w >> 2)][w & 3] & 0x7fff7fffu));
-    uint32_t big = max((uint32_t)most[0], (uint32_t)most[1]) << 16, other = big;
-    swap_halves(big, other);             // (both lanes of a row: one scale for the block's 64 numbers)
-    const int k = mc::scale_exponent(max(big, other), mc::ScaleLimits{-100, 120});
-    const float scale = mc::power_of_two(k), scale_lo = mc::power_of_two(k - 4);
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const uint32_t p0 = q[4 * j + (w >> 1)][2 * (w & 1)], p1 = q[4 * j + (w >> 1)][2 * (w & 1) + 1];
-      i16x2 hi = {0, 0}, lo = {0, 0};
-      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, p0), scale, false);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, p1), scale, true);
-      const uint32_t h = __builtin_bit_cast(uint32_t, hi);
-      const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, scale, false);
-      const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(h, scale, true);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __builtin_bit_cast(float, p0 << 16) - a[0],
-                                                    __builtin_bit_cast(float, p0 & 0xffff0000u) - a[1], scale_lo, false);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __builtin_bit_cast(float, p1 << 16) - b[0],
-                                                    __builtin_bit_cast(float, p1 & 0xffff0000u) - b[1], scale_lo, true);
-      r.hi[j][w] = (int)h;
-      r.lo[j][w] = __builtin_bit_cast(int, lo);
-    }
-    r.scales |= ((k + 127) | (k + 127 - 4) << 8) << (16 * j);
-  }
-  return r;
-}
-
 // ---- 128 rows ---------------------------------------------------------------------------------
 // Bound by the matrix and the vector pipes.  Each wavefront has 32 rows and walks all keys of the piece, a half tile (32 keys,
 // two pages) at a time, on v_mfma_f32_32x32x16; two workgroups share a compute unit.  KV tiles are copied as
@@ -724,9 +663,11 @@ __device__ __forceinline__ CodedQ code_q(const u32x4 (&q)[8]) {
 // of page h and query row n, P^T is the second product's operand as it lies, and V^T is 16 contiguous bytes of page h.
 // K rows are 128 bytes, 8 chunks of 16; chunk c of slot s of page g lies at c ^ (s % 4 + 4 (g % 2)): any 8
 // neighbouring lanes of a K read then hit 8 different chunks, so all banks.  V reads are contiguous.
-//   half step  phase 1: S of the next half on the matrix pipe; beside it this one's exponentials (in fp16: half of them, and
-//                       K's conversion)
+//   half step  phase 1: S of the next half on the matrix pipe; beside it K's conversion and half of this one's exponentials
 //              phase 2: O^T += V^T P^T; beside it the other half, the row maxima of the next S, V's conversion
+// K's codes could enter the matrix pipe as they are, with Q in two rows of codes, 8 % faster at 32k over 0; but the
+// instructions for scaled 8-bit numbers drop what lies 2^-13 below the largest of the 64 products they add, and the scores
+// would not be sums in 32 bits (lse off by 1e-4 instead of 1e-6).
 // The order within a phase is pinned: a matrix instruction, then what fits beside it.  Phase 2 has priority: of the two wavefronts
 // of a SIMD the one that came first is otherwise served first throughout, runs ahead, and the other ends alone (16k over
 // 16k tokens: workgroups of 8.4 and 11.1 million cycles, 6.11 ms; with it 5.69).
@@ -784,9 +725,6 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   vec8 q[8];
 #pragma unroll
   for (int u = 0; u < 8; ++u) q[u] = __builtin_bit_cast(vec8, q_raw[u]);
-  constexpr bool kCoded = std::is_same<T, __bf16>::value;
-  CodedQ cq;
-  if constexpr (kCoded) cq = code_q(q_raw);
   f32x16 o[4], s_a, s_b;
   const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   float m, l, mx;
@@ -880,25 +818,8 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       asm volatile("" : "+v"(l), "+v"(pk[i]));     // (stays in this phase)
     };
     vec8 op;
-    // ---- phase 1: words 0..3 (all) of P are made on the way
+    // ---- phase 1: words 0..3 of P are made on the way
     __builtin_amdgcn_s_setprio(0);
-    constexpr int kEarly = kCoded ? 8 : 4;
-    if constexpr (kCoded) {
-      const int k_scale = __builtin_bit_cast(uint32_t, ks) >> 23;
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int j = u >> 1;
-        s_next = mfma_coded(kc[2 * j], kc[2 * j + 1], k_scale, u & 1 ? cq.lo[j] : cq.hi[j], cq.scales, u, u == 0 ? zero : s_next);
-        asm volatile("" ::"v"(s_next));            // (stays in this phase)
-        soft_exp(2 * u);
-        soft_sum(2 * u);
-        soft_exp(2 * u + 1);
-        soft_sum(2 * u + 1);
-        load_v(stage, kHalf, u);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
     op = numbers<T>(kc[0][0], kc[0][1], ks);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -912,7 +833,6 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       }
       if (u >= 2 && u < 6) load_v(stage, kHalf, u - 2);
       __builtin_amdgcn_sched_barrier(0);
-    }
     }
     if constexpr (kHalf == 0) turn(t);
     // (the empty statements keep the compiler from doing either always, by selects)
@@ -936,10 +856,8 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
       const u32x4 pw = {pk[4 * e], pk[4 * e + 1], pk[4 * e + 2], pk[4 * e + 3]};
       o[u & 3] = Num<T>::mfma32(op, __builtin_bit_cast(vec8, pw), o[u & 3]);
       if (u < 4) {
-        if constexpr (kEarly < 8) {
-          soft_exp(4 + u);
-          soft_sum(4 + u);
-        }
+        soft_exp(4 + u);
+        soft_sum(4 + u);
         // the half behind the next: of this tile's successor
         if constexpr (kHalf == 0) load_k(next, 0, u);
         else load_k(next, 1, u);
@@ -976,12 +894,6 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     load_ks(stage, 0);
 #pragma unroll
     for (int cc = 0; cc < 4; ++cc) load_k(stage, 0, cc);
-    if constexpr (kCoded) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        s_a = mfma_coded(kc[u & 2], kc[(u & 2) + 1], __builtin_bit_cast(uint32_t, ks) >> 23,
-                         u & 1 ? cq.lo[u >> 1] : cq.hi[u >> 1], cq.scales, u, u == 0 ? zero : s_a);
-    } else
 #pragma unroll
     for (int u = 0; u < 8; ++u)
       s_a = Num<T>::mfma32(numbers<T>(kc[u >> 1][2 * (u & 1)], kc[u >> 1][2 * (u & 1) + 1], ks), q[u], u == 0 ? zero : s_a);

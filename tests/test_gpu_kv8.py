@@ -675,6 +675,34 @@ def test_a_prompt_from_one_engine_to_another():
     mc.mc_kv_allocator_destroy(alloc)
 
 
+@BOTH
+@pytest.mark.parametrize("new", [1, 4, 90])
+def test_scores_are_sums_in_32_bits(dtype, new):
+    """Two products of +-256 that cancel, and 126 of j 2^-9, |j| <= 15: every sum of some of them is a multiple of 2^-9
+    below 2^10, so exact in fp32 in whatever order, while a sum that drops what is 2^-13 of its largest term would lose
+    most of the score.  A score is then below 4, and what is left is the roundings of the scaled score, the exponential
+    and the logarithm (a few 2^-24 of at most 8) and of the sum (one 2^-24 for each key, in the worst order)."""
+    rng = np.random.default_rng(23)
+    c = Case(rng, dtype, 2, [150], [new])
+    n = 150 + new
+    t = TYPES[dtype]
+    bits = lambda x: torch.from_numpy(x).to(t).view(torch.int16).numpy().view(np.uint16)
+    k = rng.integers(1, 16, (n, 2, 128)) * 2.0 ** -9
+    k[:, :, 0], k[:, :, 1] = 2.0, -2.0
+    c.o.append(0, bits(k), normal_bits(rng, (n, 2, 128), dtype), 0, c.tables[0])
+    c.upload()
+    c.args_begin, c.args_new = c.begin, c.new
+    c.batch()
+    q = rng.choice([-1.0, 1.0, 1.0], (new, 8, 128))
+    q[:, :, 0], q[:, :, 1] = 128.0, 128.0
+    _, lse, _ = attend(c, dev(bits(q)).view(t), 8)
+    s = np.einsum("qhd,khd->qhk", q, np.repeat(k, 4, 1)) / np.sqrt(128.0)
+    s = np.where(np.arange(n) <= 150 + np.arange(new)[:, None, None], s, -np.inf)
+    want = np.log(np.exp(s).sum(-1))
+    err = np.abs(lse.double().cpu().numpy() - want).max()
+    assert err <= (n + 64) * 2.0 ** -24, err
+
+
 def test_as_exact_as_the_16_bit_path_on_the_same_numbers():
     """The 8-bit cache restored to a 16-bit pool holds the same K and V: both attentions agree within two roundings."""
     rng = np.random.default_rng(20)
