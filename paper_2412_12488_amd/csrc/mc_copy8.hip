@@ -70,10 +70,29 @@ __device__ __forceinline__ Rows load_rows(const char* src, int64_t row_stride, i
   return r;
 }
 
+// What a block holds that its new tokens do not replace: its scale, and of a V block this lane's columns 2 lane and
+// 2 lane + 1, 16 codes each.
+struct Held {
+  float scale;
+  u32x4 a, b;
+};
+template <bool kV>
+__device__ __forceinline__ Held load_held(const char* block, const float* scale, int lo, int hi) {
+  Held h = {0.f, {0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+  if (lo > 0) h.scale = *scale;
+  if (kV && (lo > 0 || hi < kPage)) {
+    const u32x4* columns = reinterpret_cast<const u32x4*>(block + (threadIdx.x & 63) * 32);
+    h.a = columns[0];
+    h.b = columns[1];
+  }
+  return h;
+}
+
 // One block by one wavefront: the new tokens become codes; slots [0, lo) hold codes already, at *scale, and move to the
 // new scale where the new tokens need a larger one; slots from hi on keep their bytes.
 template <typename T, bool kV>
-__device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, char* block, float* scale, ScaleLimits lim) {
+__device__ __forceinline__ void encode_block(const Rows& rows, const Held& held, int lo, int hi, char* block, float* scale,
+                                             ScaleLimits lim) {
   const int lane = threadIdx.x & 63;
   uint32_t w[16];
 #pragma unroll
@@ -81,14 +100,7 @@ __device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, c
     const int s = kV ? i : (i & ~3) + (lane >> 4);
     w[i] = s < lo || s >= hi ? 0u : rows.w[i];
   }
-  const float had = lo > 0 ? *scale : 0.f;
-  // of a V block, this lane's columns 2 lane and 2 lane + 1: 16 codes each, requested ahead of the arithmetic
-  u32x4* columns = reinterpret_cast<u32x4*>(block + lane * 32);
-  u32x4 a = {0u, 0u, 0u, 0u}, b = {0u, 0u, 0u, 0u};
-  if (kV && (lo > 0 || hi < kPage)) {
-    a = columns[0];
-    b = columns[1];
-  }
+  u32x4 a = held.a, b = held.b;
   uint32_t big = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i)
@@ -96,7 +108,7 @@ __device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, c
   int k = mc::scale_exponent(wave_max(big), lim);
   float by = 1.f;                      // old codes' factor
   if (lo > 0) {
-    const int old = mc::exponent_of(had, lim);
+    const int old = mc::exponent_of(held.scale, lim);
     k = max(k, old);
     by = mc::power_of_two(max(old - k, -126));
   }
@@ -124,6 +136,7 @@ __device__ __forceinline__ void encode_block(const Rows& rows, int lo, int hi, c
       a[j] = (na & fresh) | (oa & ~fresh);
       b[j] = (nb & fresh) | (ob & ~fresh);
     }
+    u32x4* columns = reinterpret_cast<u32x4*>(block + lane * 32);
     columns[0] = a;
     columns[1] = b;
   } else {
@@ -190,11 +203,10 @@ __device__ __forceinline__ NewToken look_up(const Append8Args& a, int g, int s) 
 
 // One workgroup: kTokens neighbouring new tokens, of which those that open a page stand for the page.  Even wavefronts
 // take K, odd ones V.
-// kTokens == 1 (batches of few tokens, where most open a page of their own: every block gets a wavefront at
-// once): blockIdx.y is a pair of heads.
-// kTokens == 64: blockIdx.y is one head, and the two wavefronts of K (V) take the pages in turns, the next one's rows
+// kTokens == 1: every token looks for itself, every block has a wavefront at once; blockIdx.y is a pair of heads.
+// kTokens > 1: blockIdx.y is one head, and the two wavefronts of K (V) take the pages in turns, the next one's memory
 // requested ahead of the present one's arithmetic.  The look-ups, five memory accesses one after the other, then serve several
-// blocks (8 prompts, 16600 tokens x 8 heads: with 16 tokens a workgroup, one or two blocks, 30.7 us).
+// blocks, but pages that get one token each are taken at a memory access's time, 2.3 us, apiece.
 template <typename T, bool kV, int kTokens>
 __device__ __forceinline__ void append_pages(const Append8Args& a, const NewToken& t, int g0, int head, int part);
 
@@ -240,32 +252,36 @@ __global__ __launch_bounds__(kThreads) void append8_kernel(Append8Args a) {
 template <typename T, bool kV, int kTokens>
 __device__ __forceinline__ void append_pages(const Append8Args& a, const NewToken& t, int g0, int head, int part) {
   struct Job {
-    int first, count, page;
+    int lo, hi;
+    char* block;
+    float* scale;
+    Rows rows;
+    Held held;
   };
   const char* from = (kV ? a.v_new : a.k_new) + ((int64_t)g0 * a.hkv + head) * kRowBytes;
   const int64_t stride = (int64_t)a.hkv * kRowBytes;
   unsigned long long open = __ballot(t.first >= 0);
-  auto take = [&](Job& j, Rows& r) __attribute__((always_inline)) {      // the next page's; false: there is none
+  auto take = [&](Job& j) __attribute__((always_inline)) {      // the next page's; false: there is none
     if (!open) return false;
     const int i = __builtin_ctzll(open);
     open &= open - 1;
     if (kTokens > 1) open &= open - 1;         // (that one is the other wavefront's)
-    j = Job{__builtin_amdgcn_readlane(t.first, i), __builtin_amdgcn_readlane(t.count, i),
-            __builtin_amdgcn_readlane(t.page, i)};
-    r = load_rows<kV>(from + i * stride, stride, j.first, j.first + j.count);
+    const int page = __builtin_amdgcn_readlane(t.page, i);
+    j.lo = __builtin_amdgcn_readlane(t.first, i);
+    j.hi = j.lo + __builtin_amdgcn_readlane(t.count, i);
+    j.block = a.codes + page * a.page_stride + (int64_t)(kV * a.hkv + head) * kBlockBytes;
+    j.scale = a.scales + ((int64_t)page * a.hkv + head) * 2 + kV;
+    j.rows = load_rows<kV>(from + i * stride, stride, j.lo, j.hi);
+    j.held = load_held<kV>(j.block, j.scale, j.lo, j.hi);
     return true;
   };
   if (kTokens > 1 && part) open &= open - 1;
   Job job, next;
-  Rows rows, next_rows;
-  bool more = take(job, rows);
+  bool more = take(job);
   while (more) {
-    more = take(next, next_rows);
-    char* block = a.codes + job.page * a.page_stride + (int64_t)(kV * a.hkv + head) * kBlockBytes;
-    float* scale = a.scales + ((int64_t)job.page * a.hkv + head) * 2 + kV;
-    encode_block<T, kV>(rows, job.first, job.first + job.count, block, scale, a.lim);
+    more = take(next);
+    encode_block<T, kV>(job.rows, job.held, job.lo, job.hi, job.block, job.scale, a.lim);
     job = next;
-    rows = next_rows;
   }
 }
 
@@ -305,9 +321,9 @@ __global__ __launch_bounds__(kThreads) void compress_kernel(Range8Args a) {
   float* scale = a.scales + layer * a.layer_scales + ((int64_t)page8 * a.hkv + head) * 2 + kv;
   const int hi = min(kPage, a.s1 - tp * kPage);
   if (kv)
-    encode_block<T, true>(load_rows<true>(src, kRowBytes, 0, hi), 0, hi, block, scale, a.lim);
+    encode_block<T, true>(load_rows<true>(src, kRowBytes, 0, hi), load_held<true>(block, scale, 0, hi), 0, hi, block, scale, a.lim);
   else
-    encode_block<T, false>(load_rows<false>(src, kRowBytes, 0, hi), 0, hi, block, scale, a.lim);
+    encode_block<T, false>(load_rows<false>(src, kRowBytes, 0, hi), load_held<false>(block, scale, 0, hi), 0, hi, block, scale, a.lim);
 }
 
 template <typename T>
@@ -505,8 +521,17 @@ mc_status convert_range(bool compress, const mc_pool_desc* pool, const mc_pool8_
   return mc::launch_status();
 }
 
-// Up to this many new tokens the append looks at them one by one: a decode batch's blocks all start at once.
-constexpr int kFewTokens = 1024;
+// How many neighbouring tokens a workgroup of the append looks at.  What counts is how many open a page: in a decode batch all,
+// in a prompt one in 16.  Measured with 8 heads, in us, with 1 / 16 / 32 tokens a workgroup:
+//   64 decode rows 5.1 / 21 / 40; 2048 of them 33 / 37 / 49; 64 sequences x 4 tokens 7.2 / 7.4 / 12, x 8 11 / 5.2 / 7.4;
+//   8 decode rows and a prompt's 100 5.2 / 14 / 14; 256 and 2048 36 / 23 / 41;
+//   prompts of 128 5.0 / 4.6 / 5.1, 512 10 / 4.8 / 5.3, 2048 31 / 5.7 / 5.8, 4096 58 / 8.7 / 7.8, 16384 219 / 26 / 21
+// The host knows the totals alone: below 4 tokens a sequence, or few altogether, one; from 32768 rows of
+// K, where the look-ups' number costs more than a decode batch among a prompt's tokens does, 32.
+int tokens_per_workgroup(int32_t batch, int32_t total_q, int32_t hkv) {
+  if (total_q <= 128 || total_q <= (int64_t)batch * 4) return 1;
+  return (int64_t)total_q * hkv <= 32768 ? 16 : 32;
+}
 
 }  // namespace
 
@@ -539,10 +564,12 @@ mc_status mc_kv8_append(const mc_pool8_desc* pool, int32_t layer, const void* k_
   a.hkv = pool->num_kv_heads;
   a.lim = mc::scale_limits(pool->dtype);
   a.skipped = pool->skipped;
-  const bool few = total_q <= kFewTokens, half = pool->dtype == MC_F16;
-  const dim3 grid(few ? total_q : (unsigned)(((int64_t)total_q + 63) / 64), few ? (a.hkv + 1) / 2 : a.hkv);
-  auto* kernel = few ? (half ? append8_kernel<_Float16, 1> : append8_kernel<__bf16, 1>)
-                     : (half ? append8_kernel<_Float16, 64> : append8_kernel<__bf16, 64>);
+  const bool half = pool->dtype == MC_F16;
+  const int tokens = tokens_per_workgroup(batch, total_q, a.hkv);
+  const dim3 grid((unsigned)(((int64_t)total_q + tokens - 1) / tokens), tokens == 1 ? (a.hkv + 1) / 2 : a.hkv);
+  auto* kernel = tokens == 1    ? (half ? append8_kernel<_Float16, 1> : append8_kernel<__bf16, 1>)
+                 : tokens == 16 ? (half ? append8_kernel<_Float16, 16> : append8_kernel<__bf16, 16>)
+                                : (half ? append8_kernel<_Float16, 32> : append8_kernel<__bf16, 32>);
   hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
   return mc::launch_status();
 }

@@ -177,6 +177,13 @@ def test_append(dtype, heads, begin, new):
     assert c.skipped.item() == 0
 
 
+@pytest.mark.parametrize("heads, begin, new", [
+    (24, [3, 0], [1100, 400]), (24, [7] * 200 + [40], [1] * 200 + [1300]), (3, [9] * 90 + [5], [1, 0, 0] * 30 + [170]),
+    (24, [5, 0, 30] * 40 + [0], [3, 0, 1] * 40 + [1500])])
+def test_append_by_workgroups_of_many_tokens(heads, begin, new):
+    test_append(kv8.BF16, heads, begin, new)
+
+
 @BOTH
 def test_append_token_by_token(dtype):
     """Scales that grow again and again, the old codes moved each time, to a factor that leaves nothing of them."""
