@@ -102,11 +102,14 @@ inline Workspace8 workspace8(int32_t batch, int32_t total_q, int G) {
 }
 
 // ---- q tiles of a sequence -----------------------------------------------------------------
-// Two kinds of plan, by the batch's sizes alone.  Batches of no more new tokens than sequences (decode steps) have
-// q tiles of at most 16 rows, whatever the sequences have, and a kernel that knows no others.  In other batches sequences
-// of at most 16 rows have one such tile and others tiles of 128 rows.
+// Two kinds of plan, by the batch's sizes alone.  Batches of no more new tokens than sequences (decode steps), and those
+// of at most 256 rows a kv head, have q tiles of at most 16 rows, whatever the sequences have, and a kernel that knows no
+// others, with its parts combined in the launch.  In other batches sequences of at most 16 rows have one such tile and others
+// tiles of 128 rows.  Plan and attention, us, of either kind (32 / 8 heads; few rows alone / both kinds):
+//   8 x 8 tokens over 4096 27 / 33, 1 x 16 over 8192 23 / 38, 1 x 32 29 / 42, 1 x 64 43 / 40, 1 x 64 over 512 22 / 25,
+//   16 decode rows and 8 tokens over 1024 20 / 25, over 8192 60 / 64; 64 x 5 over 2048 87 / 56, 64 x 16 162 / 68
 inline bool few_rows_only(int32_t batch, int32_t total_q, int G) {
-  return total_q <= batch || (int64_t)total_q * G <= kFewRows;
+  return total_q <= batch || (int64_t)total_q * G <= 16 * kFewRows;
 }
 __device__ __forceinline__ int rows_of_tiles(int q, int G, int tile_rows) {
   return (int64_t)q * G <= kFewRows ? kFewRows : tile_rows;

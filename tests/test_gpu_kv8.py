@@ -246,6 +246,15 @@ def test_attention_small(dtype, hq, hkv, begin, new):
 
 
 @BOTH
+@pytest.mark.parametrize("hq, hkv", HEADS)
+@pytest.mark.parametrize("begin, new", [
+    ([40, 500, 0, 15, 9, 300, 63], [16, 17, 5, 270, 0, 1, 2]), ([0, 62, 7], [33, 3, 229]), ([130], [64]), ([700], [65])])
+def test_attention_of_short_and_long_ranges(dtype, hq, hkv, begin, new):
+    """Q tiles of 16 and of 128 rows in one batch; batches at the border between the two kinds of plan."""
+    test_attention_small(dtype, hq, hkv, begin, new)
+
+
+@BOTH
 @pytest.mark.parametrize("hq, hkv, begin, new", [
     (8, 2, [9000], [1]), (8, 1, [5000], [7]), (4, 4, [3000, 10, 999], [1, 1, 1]),
     (8, 2, list(range(0, 2600, 13)), [1] * 200), (16, 2, [2000], [130]), (8, 2, [1500], [500]),
