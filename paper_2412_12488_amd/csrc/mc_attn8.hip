@@ -38,7 +38,7 @@ constexpr int kSpans = 512;       // workgroups of an attention launch at most: 
 constexpr int kXcds = 8;
 constexpr int kMinSpan = 4;       // units a span has at least (no fewer than a visit's) ...
 // ... and what a q tile takes beside its visits, in visits: looking it up, its Q, its first copies, its rows at the end.
-// (8 prompts of 1024..4096 tokens, with 2 / 4 / 7: 457 / 430 / 407 us; 8 decode rows, a layer, 4 / 7: 20.7 / 19.7.)
+// (8 prompts of 1024..4096 tokens, with 2 / 4 / 7 / 12: 432 / 419 / 419 / 424 us; 8 decode rows, a layer, 4 / 7: 20.7 / 19.7.)
 constexpr int kTileCost = 7;
 constexpr int kMostTokens = 1 << 30;   // of a sequence: positions stay far inside 32 bits
 constexpr int32_t kPlanMagic = 0x6d63706d;
@@ -673,7 +673,7 @@ __device__ __forceinline__ void store_block(char* to, int h, const f32x4 (&v)[4]
 // would not be sums in 32 bits (lse off by 1e-4 instead of 1e-6).
 // The order within a phase is pinned: a matrix instruction, then what fits beside it.  Phase 2 has priority: of the two wavefronts
 // of a SIMD the one that came first is otherwise served first throughout, runs ahead, and the other ends alone (16k over
-// 16k tokens: workgroups of 8.4 and 11.1 million cycles, 6.11 ms; with it 5.69).
+// 16k tokens: 6.66 ms; with it 5.92).
 template <typename T, int G>
 __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, const Target& to, char* lds) {
   typedef typename Num<T>::vec8 vec8;
@@ -878,7 +878,8 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
   };
   // One pass over the piece.  Any reference gives the same O and sum as long as nothing leaves P's range, and a reference
   // that stays at the first half tile's maximum spares the others theirs, their comparison and the exchange
-  // between lanes, a seventh of the vector instructions.  The caller looks at the sums and accumulators afterwards, and
+  // between lanes, a ninth of the vector instructions (16k over 16k tokens 5.92 ms, with one that moves 6.22; 8 prompts 419 and
+  // 439 us).  The caller looks at the sums and accumulators afterwards, and
   // repeats the pass with a reference that moves where something was lost.  (bf16 P has fp32's range; fp16 P ends at 2^16
   // above the reference, beyond which it is an infinity, and has full precision down to 2^-14 below it, as
   // with a reference that moves: that one lies at most 2^8 below the row's maximum.)
@@ -923,7 +924,7 @@ __device__ __forceinline__ void tile_piece(const Attn8Args& a, const Piece& p, c
     }
   };
   // (the repeat has a copy of the loop to itself: as a second turn of a loop around one it cost the first 26 spilled
-  // registers, and 8 prompts 417 us instead of 409)
+  // registers, and 8 prompts 2 %)
   run(true);
   {
     // A sum below 2^60 proves that no exponential was lost; an accumulator that is infinite or not a number shows here.
